@@ -75,6 +75,7 @@ extern "C" {
 #define TSD_FLAG_FUSED_DRAFT 2048u /* run the draft phase as one launch wherever that kernel is supported */
 #define TSD_FLAG_NO_WIDE_GEMM 4096u /* never use the direct-to-LDS GEMM kernels (same bits, for A/B timing) */
 #define TSD_FLAG_CLEAR_REST 8192u  /* tsd_accept_commit_static: zero the committed rows' buffer behind the round's last patch */
+#define TSD_FLAG_ROPE_INTERLEAVED 16384u /* tsd_rope_append_static: a pair is two neighbouring dims, not one of each half */
 
 typedef struct tsd_ctx tsd_ctx; /* opaque */
 
@@ -241,6 +242,93 @@ int tsd_accept_commit_static(const float* X_dev, const float* mu_q_dev, const fl
                              int32_t B, int32_t K, int32_t P, float sigma_p, float sigma_q, float fallback_r,
                              uint64_t seed, uint32_t flags, int32_t* n_acc_dev, float* commit_dev, float* ell_dev,
                              float* logu_dev, void* stream);
+
+/* ---- a round of the caller's own models ------------------------------------------------------------------------------------
+ * The three calls below are, beside tsd_accept_commit_static, what a round of a transformer that the caller runs needs: the new tokens'
+ * positions and their way into a paged cache, their attention over it, and the test of drafted tokens where the models answer with
+ * probabilities over a vocabulary.  A round of T = K + 1 tokens per sequence: per layer tsd_rope_append_static (base = tokens held),
+ * tsd_paged_attn_static (lens = base + n_new); at the end tsd_verify_tokens_static (or tsd_accept_commit_static); rolling
+ * back is holding fewer tokens: base + n_acc + 1, and what the cache has behind them is overwritten by the next round.
+ * They need no handle, allocate nothing, free nothing and keep nothing; everything is asynchronous on `stream`, whose device must be the
+ * current one, and may be captured into a graph.  Host checks come first; what only the device knows (lengths, pages, tokens) is
+ * bounded there, as said at each call, and never read or written out of range. */
+
+/* A caller's paged cache.  Token j of sequence b has its keys and values at page page_table_dev[b * table_stride + j / page_tokens], row
+ * j % page_tokens: element offset page * page_stride + row * token_stride + head * head_stride in both pools, head_dim elements in a row.
+ * A table entry outside 0 .. n_pages - 1 is a hole, and so is every token from pages_per_seq * page_tokens on: nothing is written there
+ * and no query sees it.  Pools and strides are multiples of 16 bytes. */
+typedef struct {
+  void *k_dev, *v_dev;
+  int64_t page_stride, token_stride, head_stride; /* in elements, not negative                   */
+  const int32_t* page_table_dev;                  /* [B][table_stride]                           */
+  int32_t table_stride, pages_per_seq, n_pages;
+  int32_t page_tokens; /* power of two, 1..1024        */
+  int32_t n_kv_heads;  /* 1..1024                      */
+  int32_t head_dim;    /* a multiple of 8, 8..256      */
+  int32_t dtype;       /* TSD_F32 | TSD_BF16: of the pools and of q, k, v, out */
+} tsd_paged_cache;
+
+/* Heads of new tokens: [B][T][heads][head_dim], strides in elements, a head's elements dense; data and strides are multiples of 16 bytes. */
+typedef struct {
+  void* data_dev;
+  int64_t stride_b, stride_t, stride_h;
+} tsd_rows;
+
+/* Rotary frequencies, radians per position, of pair i = 0 .. rotary_dim / 2 - 1 (rotary_dim even, 2..256), and the amplitude they go with:
+ *   TSD_ROPE_PLAIN   base^(-2i / rotary_dim), amplitude 1;
+ *   TSD_ROPE_LINEAR  the same divided by factor (positions interpolated);
+ *   TSD_ROPE_BASE    with base * factor^(R / (R - 2)), R = rotary_dim: the slowest pair interpolated by factor, the fastest kept;
+ *   TSD_ROPE_BLEND   by the turns r a pair makes over original_len positions: kept from `high` turns on, divided by factor up to `low`,
+ *                    linear in r between; amplitude 0.1 ln(factor) + 1.
+ * factor >= 1.  Host-only. */
+#define TSD_ROPE_PLAIN 0
+#define TSD_ROPE_LINEAR 1
+#define TSD_ROPE_BASE 2
+#define TSD_ROPE_BLEND 3
+int tsd_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, int32_t original_len, double low, double high,
+                         double* freq_host, double* amplitude_host);
+
+/* Rotary positions on the queries and keys of T new tokens per sequence, and the keys and values into the cache.  Token t of sequence b takes
+ * cache slot base_dev[b] + t and position positions_dev[b * T + t] (NULL: the slot).  Pair i of a head, dims (i, i + rotary_dim / 2) or,
+ * with TSD_FLAG_ROPE_INTERLEAVED, (2i, 2i + 1), turns by position * freq_dev[i] (double [rotary_dim / 2], tsd_rope_frequencies), sine and
+ * cosine times amplitude; dims from rotary_dim on stay.  The angle is taken modulo a turn in 64 bits; the rotation is fp32, rounded once.
+ * q_out may be q (in place) and must not overlap it otherwise.  n_new_dev int32 [B] (NULL: T each; clamped to 0..T): the tokens of
+ * a sequence that are there; rows behind them are neither read nor written.  Two tokens must not share a slot.  Any flag but
+ * TSD_FLAG_ROPE_INTERLEAVED is an error. */
+int tsd_rope_append_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* q_out,
+                           const tsd_rows* k, const tsd_rows* v, const int32_t* base_dev, const int32_t* n_new_dev,
+                           const int32_t* positions_dev, const double* freq_dev, int32_t rotary_dim, float amplitude, uint32_t flags,
+                           void* stream);
+
+/* Causal attention of the last n_new tokens of each sequence over the cache that holds them: token t of sequence b sees the keys
+ * j < lens_dev[b] - n_new + t + 1, out = sum_j softmax_j(scale q . k_j) v_j, query head h with key head h / (n_q_heads / n_kv_heads).
+ * n_new_dev int32 [B] (NULL: T each; clamped to 0..T); rows behind them are left as they were.  A row that sees no key (an empty
+ * sequence, holes only, scores of -inf only) gives zeros.  What the cache holds where a row does not look, not finite or never written, does not reach it.
+ * lse_dev (nullable): float [B][T][n_q_heads], the logarithm of the softmax's denominator (-inf for empty rows).
+ * max_len sizes the launch: the longest of lens_dev as far as the host knows (pages_per_seq * page_tokens does); longer sequences are
+ * right and slow.  Long caches with few rows are split over their length, and joined by a second launch: the sums of the parts go to
+ * workspace_dev (16-byte aligned, tsd_paged_attn_workspace bytes, often 0; need not be cleared; calls that may overlap need one each).
+ * bf16: products accumulate in fp32, softmax in fp32, its weights are rounded to bf16 for the product with the values.  Results depend
+ * on the sizes given, not on what runs beside: repeated calls give the same bits. */
+int tsd_paged_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, size_t* bytes_host);
+int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
+                          float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, int32_t max_len, float scale,
+                          void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Drafted tokens against the target's probabilities.  draft_dev: int32 or int64 (token_bytes 4 or 8) [B][K]; q_dev, p_dev (dtype): row i of sequence b
+ * at b * stride_b + i * stride_k elements, V probabilities each, of the draft (K rows) and of the target (K + 1 rows).  q_dev NULL: the
+ * drafts were certain (q = 1 at the draft, 0 elsewhere).  uniforms_dev: float [B][K + 1] in [0, 1).
+ *   draft i passes iff u_i q_i(x_i) < p_i(x_i); n = leading passes among the first n_draft_dev[b] (NULL: K each; clamped to 0..K) drafts;
+ *   the next token is drawn from max(p_n - q_n, 0) where draft n failed, else from p_n: the first v with w_0 + .. + w_v > u_K sum(w).
+ * Tests and sums are in 64 bits.  Rows need not sum to 1.  A weight that is not a finite positive number counts as 0; where nothing of p over
+ * q is left the draw goes by p_n, and without any weight the token is -1.  A draft outside 0 .. V - 1 fails.
+ *   n_acc_dev int32 [B]; tokens_dev [B][K + 1] of the drafts' type: the n drafts, the drawn token, -1 behind it.
+ * workspace_dev: tsd_verify_tokens_workspace bytes, 8-byte aligned, as above.  K <= 16 (TSD_E_OUT_OF_RANGE). */
+int tsd_verify_tokens_workspace(int32_t B, int32_t K, int32_t V, int32_t dtype, size_t* bytes_host);
+int tsd_verify_tokens_static(const void* draft_dev, const void* q_dev, const void* p_dev, int32_t dtype, int32_t token_bytes, int32_t B,
+                             int32_t K, int32_t V, int64_t q_stride_b, int64_t q_stride_k, int64_t p_stride_b, int64_t p_stride_k,
+                             const float* uniforms_dev, const int32_t* n_draft_dev, int32_t* n_acc_dev, void* tokens_dev,
+                             void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* tsd_draft_propose; tsd_target_verify; tsd_accept_commit(NULL).  On a non-NULL stream that is not
  * being captured by the caller, the launch sequence is captured into a HIP graph on first use and

@@ -11,7 +11,8 @@ TSD_F32, TSD_BF16 = 0, 1
 TSD_TARGET, TSD_DRAFT = 0, 1
 TSD_FLAG_SCRAMBLE_PAGES, TSD_FLAG_NO_TEMPERING, TSD_FLAG_NO_GRAPH, TSD_FLAG_NO_COMPACT, TSD_FLAG_NO_SKINNY, TSD_FLAG_SAMPLE_PROPOSALS, TSD_FLAG_NAIVE_VERIFY = 1, 2, 4, 8, 16, 32, 64
 TSD_FLAG_THRESHOLD_RULE, TSD_FLAG_BATCH_SYNC, TSD_FLAG_NO_PINNED_COUNTS, TSD_FLAG_NO_FUSED_DRAFT, TSD_FLAG_FUSED_DRAFT = 128, 256, 512, 1024, 2048
-TSD_FLAG_NO_WIDE_GEMM, TSD_FLAG_CLEAR_REST = 4096, 8192
+TSD_FLAG_NO_WIDE_GEMM, TSD_FLAG_CLEAR_REST, TSD_FLAG_ROPE_INTERLEAVED = 4096, 8192, 16384
+ROPE_SCALINGS = [None, "linear", "base", "blend"]   # TSD_ROPE_* order
 KERNEL_CLASSES = ["embed", "qkv", "attn", "resid", "gelu", "head", "accept", "route", "draft"]   # TSD_K_* order
 
 
@@ -37,6 +38,16 @@ class TsdLaunchRec(C.Structure):
                 ("K", C.c_int32), ("ms", C.c_float), ("work", C.c_double)]
 
 
+class TsdPagedCache(C.Structure):
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("page_table_dev", C.c_void_p), ("table_stride", C.c_int32), ("pages_per_seq", C.c_int32),
+                ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class TsdRows(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
 class TsdError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"libtsd error {code}: {msg}")
@@ -60,6 +71,16 @@ SYMBOLS = {
     "tsd_accept_commit_static": ([C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_float,
                                   C.c_float, C.c_float, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_void_p], C.c_int),
+    "tsd_rope_frequencies": ([C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.POINTER(C.c_double),
+                              C.POINTER(C.c_double)], C.c_int),
+    "tsd_rope_append_static": ([C.POINTER(TsdPagedCache), C.c_int32, C.c_int32, C.c_int32] + [C.POINTER(TsdRows)] * 4
+                               + [C.c_void_p] * 4 + [C.c_int32, C.c_float, C.c_uint32, C.c_void_p], C.c_int),
+    "tsd_paged_attn_workspace": ([C.POINTER(TsdPagedCache), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)], C.c_int),
+    "tsd_paged_attn_static": ([C.POINTER(TsdPagedCache), C.c_int32, C.c_int32, C.c_int32, C.POINTER(TsdRows), C.POINTER(TsdRows), C.c_void_p,
+                               C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p], C.c_int),
+    "tsd_verify_tokens_workspace": ([C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)], C.c_int),
+    "tsd_verify_tokens_static": ([C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int32] * 5 + [C.c_int64] * 4 + [C.c_void_p] * 5
+                                 + [C.c_size_t, C.c_void_p], C.c_int),
     "tsd_round": ([C.c_void_p, C.c_void_p], C.c_int),
     "tsd_run_rounds": ([C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p], C.c_int),
     "tsd_target_step": ([C.c_void_p, C.c_void_p], C.c_int),
@@ -114,7 +135,7 @@ def lib():
 
 
 def _bind_calls():
-    """Load the extension beside the library (building it first only if it does not exist) and hand it the library's entry."""
+    """Load the extension beside the library (building it first only if it does not exist) and hand it the library's entries."""
     global _calls
     handle = lib()
     from . import build as _build
@@ -123,6 +144,9 @@ def _bind_calls():
         importlib.invalidate_caches()
     from . import _torch_calls
     _torch_calls.bind(C.cast(handle.tsd_accept_commit_static, C.c_void_p).value)
+    _torch_calls.bind_round(*(C.cast(getattr(handle, name), C.c_void_p).value for name in (
+        "tsd_rope_append_static", "tsd_paged_attn_workspace", "tsd_paged_attn_static", "tsd_verify_tokens_workspace",
+        "tsd_verify_tokens_static")))
     _calls = _torch_calls
 
 
@@ -167,6 +191,61 @@ def accept_commit_static(X, mu_q, mu_p, sigma_p, sigma_q=None, rounds=None, fall
     if rc:
         _check(rc)
     return dict(n_acc=n_acc, commit=commit, ell=ell, logu=logu)
+
+
+def rope_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, original_len=0, low=1.0, high=32.0, device="cuda:0"):
+    """Rotary frequencies (float64 [rotary_dim / 2] on `device`, radians per position) and the amplitude they go with, for
+    rope_append_static.  scaling: None, "linear", "base" or "blend" (see tsd_rope_frequencies)."""
+    import torch
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {ROPE_SCALINGS}")
+    buf, amplitude = (C.c_double * max(1, rotary_dim // 2))(), C.c_double()
+    _check(lib().tsd_rope_frequencies(rotary_dim, base, ROPE_SCALINGS.index(scaling), factor, original_len, low, high, buf, C.byref(amplitude)))
+    return torch.tensor(list(buf), dtype=torch.float64, device=device), amplitude.value
+
+
+def rope_append_static(q, k, v, k_pool, v_pool, page_table, base, freq, positions=None, n_new=None, interleaved=False, amplitude=1.0, out=None):
+    """tsd_rope_append_static on torch's current stream of the tensors' device.  q: [B, T, heads, head_dim], k, v: [B, T, kv_heads, head_dim],
+    pools: [pages, page_tokens, kv_heads, head_dim], all float32 or bfloat16 with a dense last dimension and any 16-byte strides (a
+    permuted view holds a cache in another order); page_table int32 [B, pages per sequence]; base int32 [B], the tokens held so far; freq
+    from rope_frequencies; positions int32 [B, T] and n_new int32 [B] or None.  The pools are written in place; returns the rotated
+    queries: `out` (q itself to rotate in place), or a new tensor, whose rows behind n_new hold nothing."""
+    if _calls is None:
+        _bind_calls()
+    rc, out = _calls.rope_append_static(q, k, v, k_pool, v_pool, page_table, base, freq, positions, n_new, interleaved, amplitude, out)
+    if rc:
+        _check(rc)
+    return out
+
+
+def paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len=None, scale=None, n_new=None, out=None, want_lse=False):
+    """tsd_paged_attn_static on torch's current stream of the tensors' device: the last n_new (None: T each) tokens of every sequence attend
+    to the lens[b] tokens its pages hold, themselves among them.  Tensors as for rope_append_static; lens int32 [B]; max_len: the longest of lens
+    as far as the host knows (None: what the table has room for); scale: None for 1 / sqrt(head_dim).  Returns out, or (out, lse [B, T,
+    heads]) with want_lse; rows behind n_new are left as they were, in a new tensor they hold nothing.  The workspace is allocated here."""
+    if _calls is None:
+        _bind_calls()
+    if max_len is not None and max_len < 1:
+        raise ValueError("max_len must be at least 1")
+    if scale is not None and scale != scale:
+        raise ValueError("scale must be finite")
+    rc, out, lse = _calls.paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len or 0, float("nan") if scale is None else scale, n_new,
+                                            out, want_lse)
+    if rc:
+        _check(rc)
+    return (out, lse) if want_lse else out
+
+
+def verify_tokens_static(draft, q, p, uniforms, n_draft=None):
+    """tsd_verify_tokens_static on torch's current stream of the tensors' device.  draft: int32 or int64 [B, K]; q: [B, K, V] or None (certain
+    drafts), p: [B, K + 1, V], float32 or bfloat16, rows dense; uniforms: float32 [B, K + 1] in [0, 1), the last of a row for the draw;
+    n_draft: int32 [B] or None.  Returns dict(n_acc int32 [B], tokens [B, K + 1]): the drafts that passed, the drawn token, -1 behind it."""
+    if _calls is None:
+        _bind_calls()
+    rc, n_acc, tokens = _calls.verify_tokens_static(draft, q, p, uniforms, n_draft)
+    if rc:
+        _check(rc)
+    return dict(n_acc=n_acc, tokens=tokens)
 
 
 def bench_copy(dst, src):

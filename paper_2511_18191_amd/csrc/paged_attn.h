@@ -1,0 +1,160 @@
+// Attention of new tokens over a caller's paged cache: what its kernels share (paged_attn.hip on bf16 caches, paged_attn_f32.hip on fp32 ones).
+//
+// Rows: the T new tokens and the G = Hq / Hkv query heads of one key head are rows t * G + g of one product, in tiles of 16 * MT, so that a
+// key head's keys and values are read once for all of them.  Row of token t sees keys j < len - n_new + t + 1.
+//
+// Split: the keys of a sequence go in chunks of `chunk`; a workgroup takes one (sequence, key head, row tile, chunk), its wavefronts take
+// its steps of 32 keys in turn, each with a running maximum and sum of its own, joined in LDS at the end.  Where a sequence may
+// have several chunks, each leaves its rows' normalised sums and their logarithm (base 2) in the workspace, and a second launch joins those.
+#pragma once
+#include "paged_cache.h"
+
+namespace tsd {
+
+struct PagedAttnP {
+  PagedView cache;
+  RowsView q, out;
+  float* lse;        // [B][T][Hq] natural logarithms (NULL: none)
+  const int* lens;
+  const int* n_new;  // NULL: T
+  int B, T, Hq, Hkv, G, D;
+  int row_tiles, splits, chunk;
+  float scale2;      // scale * log2(e)
+  float* part_o;     // [B][splits][T][Hq][D] (splits > 1)
+  float* part_lse;   // [B][splits][T][Hq]
+};
+
+constexpr int kAttnWaves = 4;  // most wavefronts a workgroup has
+
+// launches of one type's kernels: mt row tiles of 16 a workgroup, `waves` wavefronts
+hipError_t launch_paged_attn_bf16(const PagedAttnP& p, int mt, int waves, hipStream_t st);
+hipError_t launch_paged_attn_f32(const PagedAttnP& p, int mt, int waves, hipStream_t st);
+
+#if defined(__HIPCC__)
+// What a workgroup works on.
+struct AttnWork {
+  int b, hk, tile, split;
+  int len, n_new;     // of the sequence
+  int rows;           // live rows of the key head: n_new * G
+  int row0;           // the tile's first row
+  int see_first, see_last;  // keys that the tile's first and last rows see
+  int key0, key1;     // this workgroup's keys
+  bool split_out;     // its rows' sums go to the workspace
+  bool idle;          // no rows or no chunk: nothing to write
+};
+
+// Chunks of a sequence that hold keys (at least one, which then writes the empty rows).
+__device__ __forceinline__ int attn_chunks(const PagedAttnP& p, int len) {
+  return min(p.splits, max(1, (len + p.chunk - 1) / p.chunk));
+}
+
+__device__ __forceinline__ int attn_len(const PagedAttnP& p, int b) { return min(max(p.lens[b], 0), 1 << 30); }
+__device__ __forceinline__ int attn_new(const PagedAttnP& p, int b) { return p.n_new ? min(max(p.n_new[b], 0), p.T) : p.T; }
+
+template <int TILE_ROWS>
+__device__ __forceinline__ AttnWork attn_work(const PagedAttnP& p) {
+  AttnWork w;
+  // Key heads vary fastest: workgroups go round the XCDs, so that the row tiles of a (sequence, key head) share an XCD's L2 where
+  // B * Hkv is a multiple of 8.  The last row tiles, which see the most keys, start first.
+  unsigned i = blockIdx.x;
+  const unsigned pairs = p.B * p.Hkv;
+  const unsigned pair = i % pairs;
+  i /= pairs;
+  w.split = i % p.splits;
+  w.tile = p.row_tiles - 1 - i / p.splits;
+  w.b = pair / p.Hkv;
+  w.hk = pair - w.b * p.Hkv;
+  w.len = attn_len(p, w.b);
+  w.n_new = attn_new(p, w.b);
+  w.rows = w.n_new * p.G;
+  w.row0 = w.tile * TILE_ROWS;
+  w.split_out = p.splits > 1;
+  const int chunks = attn_chunks(p, w.len);
+  w.idle = w.row0 >= w.rows || w.split >= chunks;
+  w.see_first = w.len - w.n_new + w.row0 / p.G + 1;
+  w.see_last = w.len - w.n_new + (min(w.rows, w.row0 + TILE_ROWS) - 1) / p.G + 1;
+  const int end = min(w.see_last, p.cache.cols << p.cache.pt_shift);
+  w.key0 = w.split * p.chunk;
+  // (the last chunk of the grid takes what is left, so that a length beyond max_len is slow and not wrong)
+  w.key1 = w.split == chunks - 1 ? end : min(end, w.key0 + p.chunk);
+  return w;
+}
+
+// Keys that row `row` sees (none for rows that are not there).
+__device__ __forceinline__ int attn_sees(const PagedAttnP& p, const AttnWork& w, int row) {
+  return row < w.rows ? w.len - w.n_new + row / p.G + 1 : 0;
+}
+
+// Offset of key `key`'s cache row, or -1 (see paged_row).
+__device__ __forceinline__ long attn_key_row(const PagedAttnP& p, const AttnWork& w, const int* table, int key) {
+  return key < w.key1 ? paged_row(p.cache, table, key) : -1;
+}
+
+// One step of the running softmax of a row: its lanes (q, q + 16, q + 32, q + 48) hold 8 scores each, in base 2 and -inf where the row does not
+// see the key.  Returns the factor of what was summed before; e: the weights.
+__device__ __forceinline__ float attn_running_max(const float (&s)[8], float& m_run, float (&e)[8]) {
+  float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+  mx = fmaxf(mx, __shfl_xor(mx, 16));
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  const float m_new = fmaxf(m_run, mx);
+  const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (no key seen so far: every weight is 0)
+  const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[j] - m_use);
+  m_run = m_new;
+  return alpha;
+}
+
+// Joins the wavefronts' sums of one tile of 16 rows through LDS and writes them.  O: this wavefront's sums of row `lr`, written by put(row, buf_row);
+// m, l: its running maximum and sum of the lane's row (lanes of one row agree).
+// buf: float [waves][16][DP + 4], ml: float2 [waves][16].
+template <typename T, int DP, typename Put>
+__device__ __forceinline__ void attn_join_tile(const PagedAttnP& p, const AttnWork& w, int row0, float m, float l, float* buf, float2* ml, Put put) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  constexpr int RS = DP + 4;
+  __syncthreads();
+  put(buf + (long)wave * 16 * RS, RS);
+  if (lane < 16) ml[wave * 16 + lane] = make_float2(m, l);
+  __syncthreads();
+  // a lane takes 4 dims of a row
+  constexpr int LPR = DP / 4;
+  for (int i = threadIdx.x; i < 16 * LPR; i += blockDim.x) {
+    const int lr = i / LPR, d = (i - lr * LPR) * 4, row = row0 + lr;
+    if (row >= w.rows || d >= p.D) continue;
+    float mm = -INFINITY;
+    for (int v = 0; v < waves; ++v) mm = fmaxf(mm, ml[v * 16 + lr].x);
+    float sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int v = 0; v < waves; ++v) {
+      const float2 x = ml[v * 16 + lr];
+      if (x.y == 0.f) continue;  // saw no key of this row
+      const float f = __builtin_amdgcn_exp2f(x.x - mm);
+      sum += f * x.y;
+      const f32x4 y = *reinterpret_cast<const f32x4*>(buf + ((long)v * 16 + lr) * RS + d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] += f * y[j];
+    }
+    const bool none = sum == 0.f;  // an empty row: zeros, and the logarithm of zero
+    const float inv = none ? 0.f : 1.f / sum;
+    const float lse2 = none ? -INFINITY : mm + __builtin_amdgcn_logf(sum);
+    const int t = row / p.G, h = w.hk * p.G + row - t * p.G;
+    if (w.split_out) {
+      const long r = (((long)w.b * p.splits + w.split) * p.T + t) * p.Hq + h;
+      f32x4 y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = o[j] * inv;
+      *reinterpret_cast<f32x4*>(p.part_o + r * p.D + d) = y;
+      if (d == 0) p.part_lse[r] = lse2;
+    } else {
+      typedef T T4 __attribute__((ext_vector_type(4)));
+      T4 y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = (T)(o[j] * inv);
+      *reinterpret_cast<T4*>(reinterpret_cast<T*>(p.out.p) + w.b * p.out.sb + t * p.out.st + h * p.out.sh + d) = y;
+      if (d == 0 && p.lse) p.lse[((long)w.b * p.T + t) * p.Hq + h] = lse2 * 0.69314718055994531f;
+    }
+  }
+}
+#endif
+
+}  // namespace tsd
