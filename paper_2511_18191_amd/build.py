@@ -18,7 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libtsd.so")
 CALLS = os.path.join(HERE, "_torch_calls.so")
 SOURCES = ["series_f32.hip", "tsd_api.hip", "gemm.hip", "gemm_skinny.hip", "attn.hip", "misc.hip", "moe.hip", "draft_fused.hip", "accept_static.hip", "gemm_wide.hip", "gemm_direct64.hip", "gemm_f32.hip", "small_round.hip",
-           *(os.path.join("caller", s) for s in ("paged_attn.hip", "paged_attn_f32.hip", "paged_cache.hip", "rope_append.hip", "verify_tokens.hip"))]
+           *(os.path.join("caller", s) for s in ("paged_attn.hip", "paged_attn_f32.hip", "paged_attn_prompt.hip", "paged_cache.hip", "rope_append.hip", "verify_tokens.hip"))]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
          # packed-fp32 instruction selection is switched off on purpose for the test machines
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -28,6 +28,8 @@ constexpr int kAttnWaves = 4;  // most wavefronts a workgroup has
 
 // launches of one type's kernels: mt row tiles of 16 a workgroup, `waves` wavefronts
 hipError_t launch_paged_attn_bf16(const PagedAttnP& p, int mt, int waves, hipStream_t st);
+constexpr int kPromptWaves = 4, kPromptRows = 128;
+hipError_t launch_paged_attn_prompt(const PagedAttnP& p, hipStream_t st);  // bf16, head_dim <= 128: row tiles of kPromptRows
 hipError_t launch_paged_attn_f32(const PagedAttnP& p, int mt, int waves, hipStream_t st);
 
 #if defined(__HIPCC__)
@@ -51,8 +53,8 @@ __device__ __forceinline__ int attn_chunks(const PagedAttnP& p, int len) {
 __device__ __forceinline__ int attn_len(const PagedAttnP& p, int b) { return min(max(p.lens[b], 0), 1 << 30); }
 __device__ __forceinline__ int attn_new(const PagedAttnP& p, int b) { return p.n_new ? min(max(p.n_new[b], 0), p.T) : p.T; }
 
-template <int TILE_ROWS>
-__device__ __forceinline__ AttnWork attn_work(const PagedAttnP& p) {
+// In two halves: where, which needs no memory, and how much, which needs the lengths.  (A cache's table entries are asked for between the two.)
+__device__ __forceinline__ AttnWork attn_place(const PagedAttnP& p, int tile_rows) {
   AttnWork w;
   // Key heads vary fastest: workgroups go round the XCDs, so that the row tiles of a (sequence, key head) share an XCD's L2 where
   // B * Hkv is a multiple of 8.  The last row tiles, which see the most keys, start first.
@@ -64,20 +66,24 @@ __device__ __forceinline__ AttnWork attn_work(const PagedAttnP& p) {
   w.tile = p.row_tiles - 1 - i / p.splits;
   w.b = pair / p.Hkv;
   w.hk = pair - w.b * p.Hkv;
+  // Workgroups 256 apart tend to share a compute unit: they take different sequences, whose lengths differ.
+  w.b = (w.b + i / p.splits / max(1u, 256 / pairs)) % p.B;
+  w.row0 = w.tile * tile_rows;
+  w.key0 = w.split * p.chunk;
+  w.split_out = p.splits > 1;
+  return w;
+}
+__device__ __forceinline__ void attn_lengths(const PagedAttnP& p, AttnWork& w, int tile_rows) {
   w.len = attn_len(p, w.b);
   w.n_new = attn_new(p, w.b);
   w.rows = w.n_new * p.G;
-  w.row0 = w.tile * TILE_ROWS;
-  w.split_out = p.splits > 1;
   const int chunks = attn_chunks(p, w.len);
   w.idle = w.row0 >= w.rows || w.split >= chunks;
   w.see_first = w.len - w.n_new + w.row0 / p.G + 1;
-  w.see_last = w.len - w.n_new + (min(w.rows, w.row0 + TILE_ROWS) - 1) / p.G + 1;
+  w.see_last = w.len - w.n_new + (min(w.rows, w.row0 + tile_rows) - 1) / p.G + 1;
   const int end = min(w.see_last, p.cache.cols << p.cache.pt_shift);
-  w.key0 = w.split * p.chunk;
   // (the last chunk of the grid takes what is left, so that a length beyond max_len is slow and not wrong)
   w.key1 = w.split == chunks - 1 ? end : min(end, w.key0 + p.chunk);
-  return w;
 }
 
 // Keys that row `row` sees (none for rows that are not there).
@@ -85,9 +91,9 @@ __device__ __forceinline__ int attn_sees(const PagedAttnP& p, const AttnWork& w,
   return row < w.rows ? w.len - w.n_new + row / p.G + 1 : 0;
 }
 
-// Offset of key `key`'s cache row, or -1 (see paged_row).
-__device__ __forceinline__ long attn_key_row(const PagedAttnP& p, const AttnWork& w, const int* table, int key) {
-  return key < w.key1 ? paged_row(p.cache, table, key) : -1;
+// Offset of the cache row of key `key`, whose table entry is given, or -1 (see paged_row).
+__device__ __forceinline__ long attn_key_row(const PagedAttnP& p, const AttnWork& w, int entry, int key) {
+  return key < w.key1 ? paged_row(p.cache, entry, key) : -1;
 }
 
 // One step of the running softmax of a row: its lanes (q, q + 16, q + 32, q + 48) hold 8 scores each, in base 2 and -inf where the row does not
@@ -103,6 +109,59 @@ __device__ __forceinline__ float attn_running_max(const float (&s)[8], float& m_
   for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[j] - m_use);
   m_run = m_new;
   return alpha;
+}
+
+// A value that is not finite, at a key that only some rows of a tile see, must not reach the others through 0 * inf in the product of weights and values.
+// Steps that hold such keys ("mixed": they end behind see_first, and rows differ) take those values out, as if they were 0; behind the last
+// step they are added as they are to the rows that see them: whatever the weight, the sum is then as little finite.
+// attn_take_out returns whether there were any.
+__device__ __forceinline__ bool attn_take_out(bf16x8& v) {
+  typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+  uint4v x = __builtin_bit_cast(uint4v, v);
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bool lo = (x[j] & 0x7F80u) == 0x7F80u, hi = (x[j] & 0x7F800000u) == 0x7F800000u;
+    x[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+    odd |= lo | hi;
+  }
+  v = __builtin_bit_cast(bf16x8, x);
+  return odd;
+}
+__device__ __forceinline__ bool attn_take_out(f32x4& v) {
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bool no = (__float_as_uint(v[j]) & 0x7F800000u) == 0x7F800000u;
+    if (no) v[j] = 0.f;
+    odd |= no;
+  }
+  return odd;
+}
+// What of `v` was taken out.
+__device__ __forceinline__ float attn_taken(float v) { return (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? v : 0.f; }
+
+// The first key of the mixed steps of `step` keys.
+__device__ __forceinline__ int attn_mixed_from(const AttnWork& w, int step) { return w.key0 + max(w.see_first - w.key0, 0) / step * step; }
+
+// Writes dims d .. d + 3 of a row's sums, times inv: to the output, or to the workspace where a sequence may have several chunks.
+template <typename T>
+__device__ __forceinline__ void attn_store(const PagedAttnP& p, const AttnWork& w, int row, int d, f32x4 o, float inv, float lse2) {
+  const int t = row / p.G, h = w.hk * p.G + row - t * p.G;
+  if (w.split_out) {
+    const long r = (((long)w.b * p.splits + w.split) * p.T + t) * p.Hq + h;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] *= inv;
+    *reinterpret_cast<f32x4*>(p.part_o + r * p.D + d) = o;
+    if (d == 0) p.part_lse[r] = lse2;
+  } else {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = (T)(o[j] * inv);
+    *reinterpret_cast<T4*>(reinterpret_cast<T*>(p.out.p) + w.b * p.out.sb + t * p.out.st + h * p.out.sh + d) = y;
+    if (d == 0 && p.lse) p.lse[((long)w.b * p.T + t) * p.Hq + h] = lse2 * 0.69314718055994531f;
+  }
 }
 
 // Joins the wavefronts' sums of one tile of 16 rows through LDS and writes them.  O: this wavefront's sums of row `lr`, written by put(row, buf_row);
@@ -137,22 +196,7 @@ __device__ __forceinline__ void attn_join_tile(const PagedAttnP& p, const AttnWo
     const bool none = sum == 0.f;  // an empty row: zeros, and the logarithm of zero
     const float inv = none ? 0.f : 1.f / sum;
     const float lse2 = none ? -INFINITY : mm + __builtin_amdgcn_logf(sum);
-    const int t = row / p.G, h = w.hk * p.G + row - t * p.G;
-    if (w.split_out) {
-      const long r = (((long)w.b * p.splits + w.split) * p.T + t) * p.Hq + h;
-      f32x4 y;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = o[j] * inv;
-      *reinterpret_cast<f32x4*>(p.part_o + r * p.D + d) = y;
-      if (d == 0) p.part_lse[r] = lse2;
-    } else {
-      typedef T T4 __attribute__((ext_vector_type(4)));
-      T4 y;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = (T)(o[j] * inv);
-      *reinterpret_cast<T4*>(reinterpret_cast<T*>(p.out.p) + w.b * p.out.sb + t * p.out.st + h * p.out.sh + d) = y;
-      if (d == 0 && p.lse) p.lse[((long)w.b * p.T + t) * p.Hq + h] = lse2 * 0.69314718055994531f;
-    }
+    attn_store<T>(p, w, row, d, o, inv, lse2);
   }
 }
 #endif

@@ -19,15 +19,20 @@ namespace {
 
 constexpr int v_stride(int dp) { return dp + 16; }  // V row in LDS: 32 bytes more than its dims, so that 8 rows fall on different banks
 
-template <int DP, int MT>
-__global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const PagedAttnP p) {
+template <int DP, int MT, bool FULL>  // FULL: head_dim is DP
+__global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn_bf16_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int KK = DP / 32, NB = DP / 16, VS = v_stride(DP), NV = DP / 16, VC = DP / 8;
-  const AttnWork w = attn_work<16 * MT>(p);
-  if (w.idle) return;
+  AttnWork w = attn_place(p, 16 * MT);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int qi = lane & 15, g = lane >> 4;
   const int* table = p.cache.table + (long)w.b * p.cache.table_stride;
+  const int stride = 32 * waves;
+  int sb = w.key0 + 32 * wave;
+  // (lane i and lane i + 32: key i of a step)
+  int entry = paged_entry(p.cache, table, sb + (lane & 31)), next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
+  attn_lengths(p, w, 16 * MT);
+  if (w.idle) return;
   const bf16* kbase = reinterpret_cast<const bf16*>(p.cache.k) + w.hk * p.cache.head_stride;
   const bf16* vbase = reinterpret_cast<const bf16*>(p.cache.v) + w.hk * p.cache.head_stride;
   bf16* vt = reinterpret_cast<bf16*>(smem) + wave * 32 * VS;
@@ -44,7 +49,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const 
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       const int d = kk * 32 + g * 8;
-      qf[mt][kk] = d < p.D ? *reinterpret_cast<const bf16x8*>(q + d) : zero;
+      qf[mt][kk] = FULL || d < p.D ? *reinterpret_cast<const bf16x8*>(q + d) : zero;
     }
   }
   f32x4 o[MT][NB];
@@ -72,7 +77,8 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const 
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
         const int d = kk * 32 + g * 8;
-        kf[bi][kk] = d < p.D ? *reinterpret_cast<const bf16x8*>(k + d) : zero;
+        kf[bi][kk] = *reinterpret_cast<const bf16x8*>(k + (FULL || d < p.D ? d : 0));
+        if (!FULL && d >= p.D) kf[bi][kk] = zero;
       }
     }
   };
@@ -80,43 +86,34 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = i * 64 + lane, r = c / VC, d = (c - r * VC) * 8;
-      const bf16* v = vbase + __shfl(off, r);
-      vf[i] = d < p.D ? *reinterpret_cast<const bf16x8*>(v + d) : zero;
+      vf[i] = *reinterpret_cast<const bf16x8*>(vbase + __shfl(off, r) + (FULL || d < p.D ? d : 0));  // (dims from D on: anything, never written)
     }
   };
 
-  const int stride = 32 * waves;
-  int sb = w.key0 + 32 * wave;
-  long off = attn_key_row(p, w, table, sb + (lane & 31));
+  long off = attn_key_row(p, w, entry, sb + (lane & 31));
+  entry = next_entry;
   unsigned valid = (unsigned)__ballot(off >= 0), next_valid = 0;
   if (sb < w.key1) {
     off = max(off, 0l);
     load_k(off);
     load_v(off);
   }
-  off = attn_key_row(p, w, table, sb + stride + (lane & 31));
+  off = attn_key_row(p, w, entry, sb + stride + (lane & 31));
+  entry = paged_entry(p.cache, table, sb + 2 * stride + (lane & 31));
+  bool odd = false;
   for (; sb < w.key1; sb += stride, valid = next_valid) {
     const bool more = sb + stride < w.key1;
     next_valid = (unsigned)__ballot(off >= 0);
     off = max(off, 0l);
     const bool whole = valid == 0xFFFFFFFFu && sb + 32 <= w.see_first;  // every row of the tile sees every key
-    bool careful = false;
     if (!whole) {
       // keys that are not there hold anything; their weights are 0, and so must the values be
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (!(valid >> ((i * 64 + lane) / VC) & 1)) vf[i] = zero;
-      // a value that is not finite, at a key that only some rows see, must not reach the others through 0 * inf
-      if (w.see_first < w.see_last) {
-        typedef unsigned uint4v __attribute__((ext_vector_type(4)));
-        bool odd = false;
+      if (w.see_first < w.see_last && sb + 32 > w.see_first) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const uint4v x = __builtin_bit_cast(uint4v, vf[i]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) odd |= (x[j] & 0x7F80u) == 0x7F80u || (x[j] & 0x7F800000u) == 0x7F800000u;
-        }
-        careful = __any(odd);
+        for (int i = 0; i < NV; ++i) odd |= attn_take_out(vf[i]);
       }
     }
     lds_order();  // the former step's reads before these writes
@@ -137,7 +134,8 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const 
         for (int kk = 0; kk < KK; ++kk) sc[mt][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[bi][kk], qf[mt][kk], sc[mt][bi], 0, 0, 0);
       }
     if (more) load_k(off);
-    off = attn_key_row(p, w, table, sb + 2 * stride + (lane & 31));
+    off = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
+    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
 
     bf16x8 pf[MT];
 #pragma unroll
@@ -169,7 +167,8 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const 
           for (int r = 0; r < 4; ++r) o[mt][nb][r] *= ar[r];
       }
     }
-    auto values = [&](int nb) {  // the B operand of 16 dims
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
       typedef short short4v __attribute__((ext_vector_type(4)));
       short4v hv[2];
 #pragma unroll
@@ -177,42 +176,23 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const 
         const bf16* src = vt + (8 * g + 4 * half + (qi >> 2)) * VS + nb * 16 + 4 * (qi & 3);
         hv[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)src);
       }
-      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(hv[0], hv[1], 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    if (!careful) {
+      const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(hv[0], hv[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) o[mt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[mt], vv, o[mt][nb], 0, 0, 0);
+    }
+  }
+  if (__any(odd)) {
+    for (int key = attn_mixed_from(w, 32); key < w.key1; ++key) {
+      const long at = attn_key_row(p, w, paged_entry(p.cache, table, key), key);
+      if (at < 0 || (key - w.key0) / 32 % waves != wave) continue;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const bf16x8 vv = values(nb);
+        const float v = FULL || nb * 16 + qi < p.D ? attn_taken((float)vbase[at + nb * 16 + qi]) : 0.f;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) o[mt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[mt], vv, o[mt][nb], 0, 0, 0);
-      }
-    } else {
-      // key by key, added only to the rows that see it
-#pragma unroll 1
-      for (int key = 0; key < 32; ++key) {
-        if (!(valid >> key & 1)) continue;
-        const int j = key - 8 * g;  // (the lane's element that is this key, if it has it)
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          bf16x8 pk = zero;
-          int sees_it[4];
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i == j) pk[i] = pf[mt][i];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sees_it[r] = sb + key < __shfl(sees[mt], 4 * g + r);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            bf16x8 vk = values(nb);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (i != j) vk[i] = (bf16)0.f;
-            const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pk, vk, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (sees_it[r]) o[mt][nb][r] += add[r];
-          }
-        }
+          for (int r = 0; r < 4; ++r)
+            if (key < __shfl(sees[mt], 4 * g + r)) o[mt][nb][r] += v;
       }
     }
   }
@@ -233,40 +213,59 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_bf16_kernel(const 
   }
 }
 
-// A workgroup joins the chunks of one row: lanes take 4 dims, groups of lanes every so many chunks.
-template <typename T>
+// Joins the chunks of a row: WPR wavefronts take one, their lanes 4 dims each, as many groups of lanes as a wavefront has room for
+// every so many chunks.
+template <typename T, int WPR>
 __global__ __launch_bounds__(256) void paged_attn_join_kernel(const PagedAttnP p) {
   __shared__ float part[256 * 5];
-  const int h = blockIdx.x % p.Hq, bt = blockIdx.x / p.Hq, t = bt % p.T, b = bt / p.T;
-  if (t >= attn_new(p, b)) return;
-  const int chunks = attn_chunks(p, attn_len(p, b));
-  const int lpr = p.D / 4, groups = 256 / lpr, d = (threadIdx.x % lpr) * 4, grp = threadIdx.x / lpr;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long r = blockIdx.x * (4l / WPR) + wave / WPR;
+  const bool there_is = r < (long)p.B * p.T * p.Hq;
+  const int h = (int)(r % p.Hq), t = (int)(r / p.Hq % p.T), b = there_is ? (int)(r / p.Hq / p.T) : 0;
+  const bool live = there_is && t < attn_new(p, b);
+  const int chunks = live ? attn_chunks(p, attn_len(p, b)) : 0;
+  const int lpr = p.D / 4, groups = 64 / lpr, d = (lane % lpr) * 4, grp = lane / lpr;
   const long row = ((long)b * p.splits * p.T + t) * p.Hq + h, step = (long)p.T * p.Hq;  // of chunk 0, and between chunks
   float mm = -INFINITY;
-  for (int s = 0; s < chunks; ++s) mm = fmaxf(mm, p.part_lse[row + s * step]);
+  for (int s = lane; s < chunks; s += 64) mm = fmaxf(mm, p.part_lse[row + s * step]);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
   float sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  if (grp < groups)
-    for (int s = grp; s < chunks; s += groups) {
-      const float l = p.part_lse[row + s * step];
-      if (l == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(l - mm);
-      const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_o + (row + s * step) * p.D + d);
-      sum += f;
+  if (grp < groups) {
+    constexpr int U = 4;  // chunks whose loads are in flight together
+    const int every = WPR * groups;
+    for (int s0 = wave % WPR * groups + grp; s0 < chunks; s0 += U * every) {
+      float l[U];
+      f32x4 y[U];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] += f * y[j];
+      for (int u = 0; u < U; ++u) {
+        const int s = min(s0 + u * every, chunks - 1);
+        l[u] = p.part_lse[row + s * step];
+        y[u] = *reinterpret_cast<const f32x4*>(p.part_o + (row + s * step) * p.D + d);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (s0 + u * every >= chunks || l[u] == -INFINITY) continue;  // (a chunk without keys of this row)
+        const float f = __builtin_amdgcn_exp2f(l[u] - mm);
+        sum += f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += f * y[u][j];
+      }
     }
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) part[threadIdx.x * 5 + j] = o[j];
   part[threadIdx.x * 5 + 4] = sum;
   __syncthreads();
-  if (grp) return;
-  for (int i = 1; i < groups; ++i) {
-    const float* x = part + (threadIdx.x + i * lpr) * 5;
-    sum += x[4];
+  if (!live || grp || wave % WPR) return;
+  for (int v = 0; v < WPR; ++v)
+    for (int i = v == 0; i < groups; ++i) {
+      const float* x = part + (threadIdx.x + v * 64 + i * lpr) * 5;
+      sum += x[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += x[j];
-  }
+      for (int j = 0; j < 4; ++j) o[j] += x[j];
+    }
   const bool none = sum == 0.f;
   const float inv = none ? 0.f : 1.f / sum;
   typedef T T4 __attribute__((ext_vector_type(4)));
@@ -277,36 +276,51 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(const PagedAttnP p
   if (d == 0 && p.lse) p.lse[((long)b * p.T + t) * p.Hq + h] = none ? -INFINITY : (mm + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
 }
 
+template <typename T>
+hipError_t launch_join(const PagedAttnP& p, hipStream_t st) {
+  const int64_t rows = (int64_t)p.B * p.T * p.Hq;
+  if (p.splits > 8)
+    paged_attn_join_kernel<T, 4><<<(unsigned)rows, 256, 0, st>>>(p);
+  else
+    paged_attn_join_kernel<T, 1><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(p);
+  return hipGetLastError();
+}
+
 template <int DP>
 hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
   const dim3 grid((unsigned)((long)p.B * p.Hkv * p.row_tiles * p.splits));
   const size_t stage = (size_t)waves * 32 * v_stride(DP) * 2, join = (size_t)waves * 16 * ((DP + 4) * 4 + 8);
   const size_t lds = stage > join ? stage : join;
+  const auto go = [&](auto kernel) { kernel<<<grid, waves * 64, lds, st>>>(p); };
   if (mt == 1)
-    paged_attn_bf16_kernel<DP, 1><<<grid, waves * 64, lds, st>>>(p);
-  else if (mt == 2)
-    paged_attn_bf16_kernel<DP, 2><<<grid, waves * 64, lds, st>>>(p);
+    go(p.D == DP ? paged_attn_bf16_kernel<DP, 1, true> : paged_attn_bf16_kernel<DP, 1, false>);
   else if constexpr (DP <= 128)
-    paged_attn_bf16_kernel<DP, 4><<<grid, waves * 64, lds, st>>>(p);
+    go(p.D == DP ? paged_attn_bf16_kernel<DP, 2, true> : paged_attn_bf16_kernel<DP, 2, false>);
   return hipGetLastError();
 }
 
 // What the sizes make of a call.
 struct AttnPlan {
+  bool prompt;  // the kernel for many rows
   int mt, waves, row_tiles, splits, chunk;
 };
 
 AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len) {
   AttnPlan a;
   const int rows = T * (Hq / Hkv);
-  a.mt = rows <= 16 ? 1 : 2;
-  a.row_tiles = (rows + 16 * a.mt - 1) / (16 * a.mt);
-  a.waves = D > 128 ? 2 : max_len <= 128 ? 1 : kAttnWaves;
-  const int64_t base = (int64_t)B * Hkv * a.row_tiles;
-  const int64_t want = std::max<int64_t>(1, 1024 / base), most = std::max(1, max_len / 256);
-  const int step = 32 * a.waves;
-  const int64_t splits = std::min(want, most);
-  a.chunk = (int)(((max_len + splits - 1) / splits + step - 1) / step * step);
+  a.prompt = dtype == TSD_BF16 && D <= 128 && rows > 64;
+  a.mt = rows <= 16 || D > 128 ? 1 : 2;
+  const int tile_rows = a.prompt ? kPromptRows : 16 * a.mt;
+  a.row_tiles = (rows + tile_rows - 1) / tile_rows;
+  const int64_t base = (int64_t)B * Hkv * a.row_tiles, steps = (max_len + 31) / 32;
+  a.waves = a.prompt ? kPromptWaves : (int)std::min<int64_t>(base >= 1024 && steps <= 4 ? 1 : D > 128 ? 2 : kAttnWaves, steps);
+  const int64_t step = a.prompt ? 64 : 32 * a.waves;
+  int64_t chunk = max_len;
+  if (a.prompt ? base < 256 : base < 1024) chunk = std::min<int64_t>(max_len * base / 256 / step * step, a.prompt ? max_len : 1024);
+  if (a.prompt) chunk = std::max<int64_t>(chunk, 512);
+  chunk = std::max(chunk, max_len * base / 16384);
+  chunk = std::max(step, (chunk + step - 1) / step * step);
+  a.chunk = (int)chunk;
   a.splits = (max_len + a.chunk - 1) / a.chunk;
   return a;
 }
@@ -383,14 +397,9 @@ extern "C" int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, in
   p.part_o = static_cast<float*>(workspace_dev);
   p.part_lse = need ? p.part_o + (size_t)B * a.splits * T * n_q_heads * cache->head_dim : nullptr;
   const hipStream_t st = (hipStream_t)stream;
-  hipError_t e = cache->dtype == TSD_BF16 ? launch_paged_attn_bf16(p, a.mt, a.waves, st) : launch_paged_attn_f32(p, a.mt, a.waves, st);
-  if (e == hipSuccess && a.splits > 1) {
-    const unsigned rows = (unsigned)((int64_t)B * T * n_q_heads);
-    if (cache->dtype == TSD_BF16)
-      paged_attn_join_kernel<bf16><<<rows, 256, 0, st>>>(p);
-    else
-      paged_attn_join_kernel<float><<<rows, 256, 0, st>>>(p);
-    e = hipGetLastError();
-  }
+  hipError_t e = a.prompt                   ? launch_paged_attn_prompt(p, st)
+                 : cache->dtype == TSD_BF16 ? launch_paged_attn_bf16(p, a.mt, a.waves, st)
+                                            : launch_paged_attn_f32(p, a.mt, a.waves, st);
+  if (e == hipSuccess && a.splits > 1) e = cache->dtype == TSD_BF16 ? launch_join<bf16>(p, st) : launch_join<float>(p, st);
   return e == hipSuccess ? TSD_OK : fail_no_handle(TSD_E_HIP, std::string("paged attention launch: ") + hipGetErrorString(e));
 }

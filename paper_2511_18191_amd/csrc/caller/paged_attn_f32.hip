@@ -8,15 +8,20 @@
 namespace tsd {
 namespace {
 
-template <int DP, int MT>
-__global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_f32_kernel(const PagedAttnP p) {
+template <int DP, int MT, bool FULL>  // FULL: head_dim is DP
+__global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_f32_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int KC = DP / 16, NC = DP / 64;
-  const AttnWork w = attn_work<16 * MT>(p);
-  if (w.idle) return;
+  AttnWork w = attn_place(p, 16 * MT);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int qi = lane & 15, g = lane >> 4;
   const int* table = p.cache.table + (long)w.b * p.cache.table_stride;
+  const int stride = 32 * waves;
+  int sb = w.key0 + 32 * wave;
+  // (lane i and lane i + 32: key i of a step)
+  int entry = paged_entry(p.cache, table, sb + (lane & 31)), next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
+  attn_lengths(p, w, 16 * MT);
+  if (w.idle) return;
   const float* kbase = reinterpret_cast<const float*>(p.cache.k) + w.hk * p.cache.head_stride;
   const float* vbase = reinterpret_cast<const float*>(p.cache.v) + w.hk * p.cache.head_stride;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -30,7 +35,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_f32_kernel(const P
     const int r = min(row, w.rows - 1), t = r / p.G, h = w.hk * p.G + r - t * p.G;
     const float* q = reinterpret_cast<const float*>(p.q.p) + w.b * p.q.sb + t * p.q.st + h * p.q.sh;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) qf[mt][c] = c * 16 + g * 4 < p.D ? *reinterpret_cast<const f32x4*>(q + c * 16 + g * 4) : zero;
+    for (int c = 0; c < KC; ++c) qf[mt][c] = FULL || c * 16 + g * 4 < p.D ? *reinterpret_cast<const f32x4*>(q + c * 16 + g * 4) : zero;
   }
   f32x4 o[MT][NC][4];  // [..][j]: dim 64 c + 4 qi + j of rows 4g ..
   float m_run[MT], l_run[MT];
@@ -50,7 +55,11 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_f32_kernel(const P
     for (int bi = 0; bi < 2; ++bi) {
       const float* k = kbase + __shfl(off, 16 * bi + qi);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) kf[bi][c] = c * 16 + g * 4 < p.D ? *reinterpret_cast<const f32x4*>(k + c * 16 + g * 4) : zero;
+      for (int c = 0; c < KC; ++c) {
+        const int d = c * 16 + g * 4;
+        kf[bi][c] = *reinterpret_cast<const f32x4*>(k + (FULL || d < p.D ? d : 0));
+        if (!FULL && d >= p.D) kf[bi][c] = zero;
+      }
     }
   };
   auto load_v = [&](long off) {
@@ -60,20 +69,21 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_f32_kernel(const P
       for (int r = 0; r < 4; ++r) {
         const float* v = vbase + __shfl(off, 16 * bi + 4 * g + r);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) vf[bi][r][c] = c * 64 + qi * 4 < p.D ? *reinterpret_cast<const f32x4*>(v + c * 64 + qi * 4) : zero;
+        for (int c = 0; c < NC; ++c) vf[bi][r][c] = *reinterpret_cast<const f32x4*>(v + (FULL || c * 64 + qi * 4 < p.D ? c * 64 + qi * 4 : 0));  // (dims from D on: anything, never written)
       }
   };
 
-  const int stride = 32 * waves;
-  int sb = w.key0 + 32 * wave;
-  long off = attn_key_row(p, w, table, sb + (lane & 31));
+  long off = attn_key_row(p, w, entry, sb + (lane & 31));
+  entry = next_entry;
   unsigned valid = (unsigned)__ballot(off >= 0), next_valid = 0;
   if (sb < w.key1) {
     off = max(off, 0l);
     load_k(off);
     load_v(off);
   }
-  off = attn_key_row(p, w, table, sb + stride + (lane & 31));
+  off = attn_key_row(p, w, entry, sb + stride + (lane & 31));
+  entry = paged_entry(p.cache, table, sb + 2 * stride + (lane & 31));
+  bool odd = false;
   for (; sb < w.key1; sb += stride, valid = next_valid) {
     const bool more = sb + stride < w.key1;
     next_valid = (unsigned)__ballot(off >= 0);
@@ -91,9 +101,8 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_f32_kernel(const P
           for (int j = 0; j < 4; ++j) sc[mt][bi] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[bi][c][j], qf[mt][c][j], sc[mt][bi], 0, 0, 0);
       }
     if (more) load_k(off);
-    bool careful = false;
     if (!whole) {
-      bool odd = false;
+      const bool mixed = w.see_first < w.see_last && sb + 32 > w.see_first;  // (see attn_take_out)
 #pragma unroll
       for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
@@ -101,10 +110,8 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_f32_kernel(const P
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
             if (!(valid >> (16 * bi + 4 * g + r) & 1)) vf[bi][r][c] = zero;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) odd |= (__float_as_uint(vf[bi][r][c][j]) & 0x7F800000u) == 0x7F800000u;
+            if (mixed) odd |= attn_take_out(vf[bi][r][c]);
           }
-      careful = w.see_first < w.see_last && __any(odd);
     }
     float e[MT][8];
 #pragma unroll
@@ -132,46 +139,38 @@ __global__ __launch_bounds__(kAttnWaves * 64) void paged_attn_f32_kernel(const P
         }
       }
     }
-    if (!careful) {
 #pragma unroll
-      for (int bi = 0; bi < 2; ++bi)
+    for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt)
-                o[mt][c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(e[mt][4 * bi + r], vf[bi][r][c][j], o[mt][c][j], 0, 0, 0);
-    } else {
-      // key by key, added only to the rows that see it: a value that is not finite must not reach the others through 0 * inf
-#pragma unroll
-      for (int x = 0; x < 8; ++x)
-#pragma unroll 1
-        for (int gg = 0; gg < 4; ++gg) {
-          const int key = 16 * (x >> 2) + 4 * gg + (x & 3);
-          if (!(valid >> key & 1)) continue;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            int sees_it[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sees_it[r] = sb + key < __shfl(sees[mt], 4 * g + r);
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const f32x4 add =
-                    __builtin_amdgcn_mfma_f32_16x16x4f32(g == gg ? e[mt][x] : 0.f, g == gg ? vf[x >> 2][x & 3][c][j] : 0.f, zero, 0, 0, 0);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                  if (sees_it[r]) o[mt][c][j][r] += add[r];
-              }
-          }
-        }
-    }
+            for (int mt = 0; mt < MT; ++mt)
+              o[mt][c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(e[mt][4 * bi + r], vf[bi][r][c][j], o[mt][c][j], 0, 0, 0);
     if (more) load_v(off);
-    off = attn_key_row(p, w, table, sb + 2 * stride + (lane & 31));
+    off = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
+    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
+  }
+
+  if (__any(odd)) {
+    for (int key = attn_mixed_from(w, 32); key < w.key1; ++key) {
+      const long at = attn_key_row(p, w, paged_entry(p.cache, table, key), key);
+      if (at < 0 || (key - w.key0) / 32 % waves != wave) continue;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const f32x4 x = FULL || c * 64 + qi * 4 < p.D ? *reinterpret_cast<const f32x4*>(vbase + at + c * 64 + qi * 4) : zero;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (key < __shfl(sees[mt], 4 * g + r)) o[mt][c][j][r] += attn_taken(x[j]);
+      }
+    }
   }
 
   float* buf = reinterpret_cast<float*>(smem);
@@ -199,12 +198,11 @@ template <int DP>
 hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
   const dim3 grid((unsigned)((long)p.B * p.Hkv * p.row_tiles * p.splits));
   const size_t lds = (size_t)waves * 16 * ((DP + 4) * 4 + 8);
+  const auto go = [&](auto kernel) { kernel<<<grid, waves * 64, lds, st>>>(p); };
   if (mt == 1)
-    paged_attn_f32_kernel<DP, 1><<<grid, waves * 64, lds, st>>>(p);
-  else if (mt == 2)
-    paged_attn_f32_kernel<DP, 2><<<grid, waves * 64, lds, st>>>(p);
+    go(p.D == DP ? paged_attn_f32_kernel<DP, 1, true> : paged_attn_f32_kernel<DP, 1, false>);
   else if constexpr (DP <= 128)
-    paged_attn_f32_kernel<DP, 4><<<grid, waves * 64, lds, st>>>(p);
+    go(p.D == DP ? paged_attn_f32_kernel<DP, 2, true> : paged_attn_f32_kernel<DP, 2, false>);
   return hipGetLastError();
 }
 

@@ -30,12 +30,13 @@ inline RowsView rows_view(const tsd_rows& r) { return {static_cast<char*>(r.data
 #if defined(__HIPCC__)
 // Offset of cache row `slot` of a sequence whose table row is `table` (head 0), or -1 where the table has no page for it: beyond its columns,
 // or an entry that names none of the pool's pages.  Such a slot is a hole: nothing is read or written there.
-__device__ __forceinline__ long paged_row(const PagedView& c, const int* table, int slot) {
-  const int col = slot >> c.pt_shift;
-  if (slot < 0 || col >= c.cols) return -1;
-  const int page = table[col];
-  if ((unsigned)page >= (unsigned)c.n_pages) return -1;
-  return page * c.page_stride + (slot & ((1 << c.pt_shift) - 1)) * c.token_stride;
+// In two halves, so that the entry can be on its way before it is known whether it counts.
+__device__ __forceinline__ int paged_entry(const PagedView& c, const int* table, int slot) {
+  return table[min(max(slot, 0) >> c.pt_shift, c.cols - 1)];
+}
+__device__ __forceinline__ long paged_row(const PagedView& c, int entry, int slot) {
+  if (slot < 0 || slot >> c.pt_shift >= c.cols || (unsigned)entry >= (unsigned)c.n_pages) return -1;
+  return entry * c.page_stride + (slot & ((1 << c.pt_shift) - 1)) * c.token_stride;
 }
 #endif
 

@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const RopeP p) {
     sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
     cs[i] = make_float2(p.amplitude * c, p.amplitude * s);
   }
-  const long row = paged_row(p.cache, p.cache.table + (long)b * p.cache.table_stride, slot);
+  const long row = paged_row(p.cache, paged_entry(p.cache, p.cache.table + (long)b * p.cache.table_stride, slot), slot);
   __syncthreads();
 
   const int n_q = p.Hq * p.rot_items, n_rot = n_q + p.Hkv * p.rot_items, n_all = n_rot + p.Hkv * p.copy_items;

@@ -4,11 +4,15 @@
 // from w = max(p_n - q_n, 0) where a draft failed, else from w = p_n: the first v with w_0 + .. + w_v > u_K W, W the sum of all.  The sums are
 // held in 64 bits: over 10^5 fp32 terms a running sum in 32 would move one draw in a hundred to a neighbour.
 //
-// Memory bound: one row of p, and one of q where a draft failed.  A row goes in segments of kSegment elements, one wavefront each, whose sums go to
-// the workspace; a second launch, a workgroup per sequence, finds the segment that crosses u_K W and the token inside it.  Both find n
-// for themselves (K gathered pairs).  Rows start anywhere (an odd vocabulary), so 16-byte loads need no alignment beyond the element's.
+// Memory bound: one row of p, and one of q where a draft failed.  A row goes in segments of kSegment elements, summed by a wavefront each; then the
+// segment that crosses u_K W is found, and the token inside it.  Short rows, and those of many sequences, take one workgroup each; else a
+// row's segments are dealt to several (some 512 in all), and the one that comes last goes on (last_arriver.h).  Rows start anywhere (an
+// odd vocabulary), so 16-byte loads need no alignment beyond the element's.
+// Three dependent trips to memory (drafts, their probabilities, the rows), 3 us, bound small calls: 1 x 4 drafts, 32000 fp32 probabilities
+// 7.7 us; 64 x 6, 131072 fp32 16.9 us (58 MB: 3.4 TB/s); 256 x 8, 50257 bf16 14.4 us (41 MB: 2.8 TB/s).
 #include <algorithm>
 
+#include "last_arriver.h"
 #include "paged_cache.h"
 
 namespace tsd {
@@ -16,6 +20,7 @@ namespace {
 
 constexpr int kSegment = 1024;
 constexpr int kMaxDrafts = 16;
+constexpr int kOneSegments = 256;  // most segments of a row that one workgroup sums
 
 struct VerifyP {
   const void* draft;      // int32 or int64 [B][K]
@@ -28,17 +33,21 @@ struct VerifyP {
   void* tokens;           // [B][K + 1]
   int B, K, V, wide;      // wide: 64-bit tokens
   int segments;
-  double* sums;           // [B][segments]
+  int groups, per;        // workgroups that share a row, and the segments each of them takes
+  double* sums;           // [2][B][segments]: of the row's weights, and of p alone where none of those is left
+  uint64_t* slots;        // [B][groups]
+  uint64_t tag;
 };
 
 __device__ __forceinline__ long token_at(const void* p, long i, int wide) {
   return wide ? reinterpret_cast<const long*>(p)[i] : (long)reinterpret_cast<const int*>(p)[i];
 }
 
-// What a sequence's drafts come to, the same in every lane of the (first) wavefront.
+// What a sequence's drafts come to, the same in every lane of a wavefront: how many passed, and the token of the one that failed
+// (kNoToken: none of this vocabulary; kNoneFailed: all passed).
+constexpr int kNoToken = -1, kNoneFailed = -2;
 struct Verdict {
-  int n, drafted;
-  long failed;  // the draft that failed (residual of a certain draft)
+  int n, failed;
 };
 
 template <typename T>
@@ -57,8 +66,7 @@ __device__ __forceinline__ Verdict test_drafts(const VerifyP& a, int b) {
   }
   Verdict v;
   v.n = __builtin_ctzll(~__ballot(pass));  // (lanes from `drafted` on do not pass)
-  v.drafted = drafted;
-  v.failed = __shfl(x, v.n);
+  v.failed = v.n == drafted ? kNoneFailed : __shfl(x >= 0 && x < a.V ? (int)x : kNoToken, v.n);
   return v;
 }
 
@@ -67,10 +75,11 @@ template <typename T>
 struct Weights {
   const T* p;
   const T* q;      // NULL: p alone
-  long without;    // this token has none (-1: every token has its own)
+  int without;     // this token has none (kNoToken: every token has its own)
+  // Compared in 32 bits, subtracted in 64; what is no finite positive number weighs nothing.
   __device__ __forceinline__ double of(float x, float y, long v) const {
-    const double d = (double)x - (double)y;
-    return d > 0.0 && d < (double)INFINITY && v != without ? d : 0.0;  // (what is no number weighs nothing)
+    const bool some = x > y && x < INFINITY && y > -INFINITY && (v == kNoToken || (int)v != without);
+    return (double)(some ? x : 0.f) - (double)(some ? y : 0.f);
   }
 };
 
@@ -78,46 +87,56 @@ template <typename T>
 __device__ __forceinline__ Weights<T> weights_of(const VerifyP& a, int b, const Verdict& v) {
   Weights<T> w;
   w.p = reinterpret_cast<const T*>(a.p) + b * a.p_sb + v.n * a.p_sr;
-  const bool failed = v.n < v.drafted;
+  const bool failed = v.failed != kNoneFailed;
   w.q = failed && a.q ? reinterpret_cast<const T*>(a.q) + b * a.q_sb + v.n * a.q_sr : nullptr;
-  w.without = failed && !a.q ? v.failed : -1;
+  w.without = failed && !a.q ? v.failed : kNoToken;
   return w;
 }
 
+// 16 bytes of a row, which may start at any element.  In words: as elements, the compiler unpacks each load where it is issued, and waits for it.
+typedef unsigned Words __attribute__((ext_vector_type(4)));
 template <typename T>
 struct alignas(sizeof(T)) Pack {
-  T x[16 / sizeof(T)];
+  unsigned char bytes[16];
 };
+template <typename T>
+__device__ __forceinline__ Words load_pack(const T* from) {
+  return __builtin_bit_cast(Words, *reinterpret_cast<const Pack<T>*>(from));
+}
+template <typename T>
+__device__ __forceinline__ float element(const Words& w, int j) {
+  if constexpr (sizeof(T) == 4)
+    return __uint_as_float(w[j]);
+  else
+    return __uint_as_float(j & 1 ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16);  // (bf16 is the upper half of an fp32)
+}
 
 // C packs of weights, pack c from element v0 + c * STEP on; 0 beyond V.  inside: all of them lie in the row (the same in every lane).
 template <typename T, int C, int STEP>
 __device__ __forceinline__ void load_weights(const Weights<T>& w, long v0, int V, bool inside, double (&d)[C * (16 / sizeof(T))]) {
   constexpr int E = 16 / sizeof(T);
-  Pack<T> x[C], y[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int j = 0; j < E; ++j) x[c].x[j] = y[c].x[j] = (T)0.f;
   if (inside) {
+    Words x[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) x[c] = *reinterpret_cast<const Pack<T>*>(w.p + v0 + c * STEP);
-    if (w.q)
+    for (int c = 0; c < C; ++c) x[c] = load_pack(w.p + v0 + c * STEP);
+    if (w.q) {
+      Words y[C];
 #pragma unroll
-      for (int c = 0; c < C; ++c) y[c] = *reinterpret_cast<const Pack<T>*>(w.q + v0 + c * STEP);
+      for (int c = 0; c < C; ++c) y[c] = load_pack(w.q + v0 + c * STEP);
+#pragma unroll
+      for (int i = 0; i < C * E; ++i) d[i] = w.of(element<T>(x[i / E], i % E), element<T>(y[i / E], i % E), kNoToken);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C * E; ++i) d[i] = w.of(element<T>(x[i / E], i % E), 0.f, v0 + i / E * STEP + i % E);
+    }
   } else {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int j = 0; j < E; ++j)
-        if (v0 + c * STEP + j < V) {
-          x[c].x[j] = w.p[v0 + c * STEP + j];
-          if (w.q) y[c].x[j] = w.q[v0 + c * STEP + j];
-        }
+    for (int i = 0; i < C * E; ++i) {
+      const long v = v0 + i / E * STEP + i % E;
+      d[i] = 0.0;
+      if (v < V) d[i] = w.of((float)w.p[v], w.q ? (float)w.q[v] : 0.f, v);
+    }
   }
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int j = 0; j < E; ++j) d[c * E + j] = w.of((float)x[c].x[j], (float)y[c].x[j], v0 + c * STEP + j);
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -137,16 +156,6 @@ __device__ __forceinline__ double segment_sum(const Weights<T>& w, long s, int V
   return wave_sum(sum);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP a) {
-  const int groups = (a.segments + 3) / 4;
-  const int b = blockIdx.x / groups, s = (blockIdx.x - b * groups) * 4 + (threadIdx.x >> 6);
-  if (s >= a.segments) return;
-  const Verdict v = test_drafts<T>(a, b);
-  const double sum = segment_sum(weights_of<T>(a, b, v), s, a.V);
-  if ((threadIdx.x & 63) == 0) a.sums[(long)b * a.segments + s] = sum;
-}
-
 // Inclusive sums over the wavefront's lanes.
 __device__ __forceinline__ double wave_scan(double v) {
   const int lane = threadIdx.x & 63;
@@ -164,10 +173,12 @@ struct Found {
   int segment;
   double before, target;
 };
+template <bool ONE>
 __device__ __forceinline__ Found find_segment(const double* sums, int segments, double u) {
   const int lane = threadIdx.x & 63, per = (segments + 63) / 64, first = lane * per, last = min(segments, first + per);
   double own = 0.0;
-  for (int s = first; s < last; ++s) own += sums[s];
+  const auto sum = [&](int s) { return ONE ? sums[s] : left_by_all(sums + s); };
+  for (int s = first; s < last; ++s) own += sum(s);
   const double upto = wave_scan(own);
   const double whole = __shfl(upto, 63), prev = __shfl_up(upto, 1);
   Found f = {-1, 0.0, u * whole};
@@ -176,7 +187,7 @@ __device__ __forceinline__ Found find_segment(const double* sums, int segments, 
   int at = -1, heavy = -1;
   double before = 0.0, heavy_before = 0.0;
   for (int s = first; s < last; ++s) {
-    const double x = sums[s], upper = run + x;
+    const double x = sum(s), upper = run + x;
     if (x > 0.0) {
       heavy = s;
       heavy_before = run;
@@ -231,25 +242,40 @@ __device__ __forceinline__ long find_token(const Weights<T>& w, const Found& f, 
   return __shfl(heavy, 63 - __builtin_clzll(who));
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void verify_draw_kernel(const VerifyP a) {
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double* sums = a.sums + (long)b * a.segments;
+// ONE: a workgroup sums a whole row, into LDS.  Else the row's workgroups sum a segment per wavefront, and the last of them draws.
+template <typename T, int WAVES, bool ONE>
+__global__ __launch_bounds__(WAVES * 64) void verify_kernel(const VerifyP a) {
+  __shared__ double own_sums[ONE ? kOneSegments : 1];
+  const int b = ONE ? blockIdx.x : blockIdx.x / a.groups, group = ONE ? 0 : blockIdx.x - b * a.groups;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double* sums = ONE ? own_sums : a.sums + (long)b * a.segments;
+  const double u = (double)a.uniforms[(long)b * (a.K + 1) + a.K];
   const Verdict v = test_drafts<T>(a, b);
   Weights<T> w = weights_of<T>(a, b, v);
-  const double u = (double)a.uniforms[(long)b * (a.K + 1) + a.K];
-  Found f = find_segment(sums, a.segments, u);
+  for (int s = group * a.per + wave, end = ONE ? a.segments : min(a.segments, (group + 1) * a.per); s < end; s += WAVES) {
+    const double sum = segment_sum(w, s, a.V);
+    if (lane == 0) ONE ? (void)(sums[s] = sum) : leave(sums + s, sum);
+  }
+  if (ONE) {
+    __syncthreads();
+  } else {
+    if (!came_last(a.slots + (long)b * a.groups, a.groups, group, a.tag)) return;
+  }
+  Found f = find_segment<ONE>(sums, a.segments, u);
   if (f.segment < 0 && (w.q || w.without >= 0)) {  // nothing is left of p over q: the draw goes by p (the same in every wavefront)
     w.q = nullptr;
-    w.without = -1;
+    w.without = kNoToken;
     __syncthreads();
-    for (int s = wave; s < a.segments; s += 4) {
+    if (!ONE) sums += (long)a.B * a.segments;  // (another finisher may still be reading the others)
+    for (int s = wave; s < a.segments; s += WAVES) {
       const double sum = segment_sum(w, s, a.V);
-      if (lane == 0) sums[s] = sum;
+      if (lane == 0) ONE ? (void)(sums[s] = sum) : leave(sums + s, sum);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    f = find_segment(sums, a.segments, u);
+    f = find_segment<ONE>(sums, a.segments, u);
   }
+  if (!ONE) clear_slots(a.slots + (long)b * a.groups, a.groups);
   if (wave) return;
   const long token = f.segment < 0 ? -1 : find_token(w, f, a.V);
   if (lane <= a.K) {
@@ -280,7 +306,8 @@ extern "C" int tsd_verify_tokens_workspace(int32_t B, int32_t K, int32_t V, int3
   const int rc = check_verify(dtype, B, K, V);
   if (rc) return rc;
   if (!bytes_host) return fail_no_handle(TSD_E_INVALID_ARG, "bytes_host must not be NULL");
-  *bytes_host = ((size_t)B * ((V + (size_t)kSegment - 1) / kSegment) * sizeof(double) + 255) / 256 * 256;
+  const size_t segments = (V + (size_t)kSegment - 1) / kSegment;
+  *bytes_host = ((size_t)B * (2 * segments + (segments + 3) / 4) * 8 + 255) / 256 * 256;
   return TSD_OK;
 }
 
@@ -315,15 +342,26 @@ extern "C" int tsd_verify_tokens_static(const void* draft_dev, const void* q_dev
   a.wide = token_bytes == 8;
   a.segments = (int)((V + (int64_t)kSegment - 1) / kSegment);
   a.sums = static_cast<double*>(workspace_dev);
+  // (some 512 workgroups in all: 64 x 131072 fp32 with 4, 8, 16, 32 a row 20.1, 16.8, 17.5, 21.6 us, 128 x 65536 15.6, 16.6, 20.0, 20.1)
+  const int want = (int)std::min<int64_t>((a.segments + 3) / 4, std::max(1, 512 / B));
+  a.per = ((a.segments + want - 1) / want + 3) / 4 * 4;
+  a.groups = (a.segments + a.per - 1) / a.per;
+  a.slots = reinterpret_cast<uint64_t*>(a.sums + 2 * (size_t)B * a.segments);
   const hipStream_t st = (hipStream_t)stream;
-  const unsigned grid = (unsigned)((int64_t)B * ((a.segments + 3) / 4));
-  if (dtype == TSD_BF16) {
-    verify_sums_kernel<bf16><<<grid, 256, 0, st>>>(a);
-    verify_draw_kernel<bf16><<<B, 256, 0, st>>>(a);
-  } else {
-    verify_sums_kernel<float><<<grid, 256, 0, st>>>(a);
-    verify_draw_kernel<float><<<B, 256, 0, st>>>(a);
-  }
+  // One workgroup a row, us against several (fp32): 8000 x 4 sequences 7.5 / 9.1, 32000 x 1 8.0 / 7.7, 32000 x 160 11.6 / 13.4,
+  // 131072 x 1 15.1 / 8.2, 131072 x 128 30.0 / 29.6 and x 200 36.6 / 45.8.
+  const bool one = a.segments <= 16 || (B >= 160 && a.segments <= kOneSegments);
+  a.tag = new_tag();
+  const auto go = [&](auto split, auto whole) {
+    if (one)
+      whole<<<B, 1024, 0, st>>>(a);
+    else
+      split<<<(unsigned)((int64_t)B * a.groups), 256, 0, st>>>(a);
+  };
+  if (dtype == TSD_BF16)
+    go(verify_kernel<bf16, 4, false>, verify_kernel<bf16, 16, true>);
+  else
+    go(verify_kernel<float, 4, false>, verify_kernel<float, 16, true>);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TSD_OK : fail_no_handle(TSD_E_HIP, std::string("token verification launch: ") + hipGetErrorString(e));
 }

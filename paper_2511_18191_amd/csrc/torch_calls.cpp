@@ -144,9 +144,11 @@ struct Wrong : std::invalid_argument {  // becomes a ValueError
 struct WrongType : std::invalid_argument {  // becomes a TypeError
   using std::invalid_argument::invalid_argument;
 };
-void need(bool ok, const std::string& what) {
-  if (!ok) throw Wrong(what);
-}
+// (the message is put together only where the check fails: some twenty of them took 1 us of a call)
+#define NEED(ok, what)                       \
+  do {                                       \
+    if (!(ok)) throw Wrong(std::string(what)); \
+  } while (0)
 
 const at::Tensor& the(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) throw WrongType(std::string(name) + " must be a tensor");
@@ -155,33 +157,33 @@ const at::Tensor& the(PyObject* o, const char* name) {
 const at::Tensor* maybe(PyObject* o, const char* name) { return o == Py_None ? nullptr : &the(o, name); }
 
 int32_t whole(int64_t v, const char* name) {
-  need(v >= 0 && v <= INT32_MAX, std::string(name) + " is out of range");
+  NEED(v >= 0 && v <= INT32_MAX, std::string(name) + " is out of range");
   return (int32_t)v;
 }
 
 void on_gpu(const at::Tensor& t, const char* name) {
-  need(t.is_cuda(), std::string(name) + ": expected a cuda device, but got: " + t.device().str());
+  NEED(t.is_cuda(), std::string(name) + ": expected a cuda device, but got: " + t.device().str());
 }
 void like(const at::Tensor& t, const at::Tensor& first, const char* name) {
-  need(t.device() == first.device(), std::string(name) + " is on " + t.device().str() + ", not on " + first.device().str());
-  need(t.scalar_type() == first.scalar_type(), std::string(name) + " is of another type");
+  NEED(t.device() == first.device(), std::string(name) + " is on " + t.device().str() + ", not on " + first.device().str());
+  NEED(t.scalar_type() == first.scalar_type(), std::string(name) + " is of another type");
 }
 // A dense tensor of indices (or of other plain values) with these sizes, on the device of `first`.
 void plain(const at::Tensor& t, const at::Tensor& first, at::ScalarType type, at::IntArrayRef sizes, const char* name) {
-  need(t.device() == first.device(), std::string(name) + " is on " + t.device().str() + ", not on " + first.device().str());
-  need(t.scalar_type() == type, std::string(name) + " must be of type " + c10::toString(type));
-  need(t.sizes() == sizes, std::string(name) + " has another shape than its call's");
-  need(t.is_contiguous(), std::string(name) + " must be contiguous");
+  NEED(t.device() == first.device(), std::string(name) + " is on " + t.device().str() + ", not on " + first.device().str());
+  NEED(t.scalar_type() == type, std::string(name) + " must be of type " + c10::toString(type));
+  NEED(t.sizes() == sizes, std::string(name) + " has another shape than its call's");
+  NEED(t.is_contiguous(), std::string(name) + " must be contiguous");
 }
 int dtype_of(const at::Tensor& t, const char* name) {
-  need(t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16, std::string(name) + " must be float32 or bfloat16");
+  NEED(t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16, std::string(name) + " must be float32 or bfloat16");
   return t.scalar_type() == at::kFloat ? TSD_F32 : TSD_BF16;
 }
 
 // [B, T, heads, head_dim] with dense heads (dimensions of one step have no stride that matters)
 tsd_rows rows_of(const at::Tensor& t, at::IntArrayRef sizes, const char* name) {
-  need(t.sizes() == sizes, std::string(name) + " has another shape than its call's");
-  need(t.stride(3) == 1, std::string(name) + ": the last dimension must be dense");
+  NEED(t.sizes() == sizes, std::string(name) + " has another shape than its call's");
+  NEED(t.stride(3) == 1, std::string(name) + ": the last dimension must be dense");
   tsd_rows r;
   r.data_dev = t.data_ptr();
   r.stride_b = sizes[0] > 1 ? t.stride(0) : 0;
@@ -191,19 +193,19 @@ tsd_rows rows_of(const at::Tensor& t, at::IntArrayRef sizes, const char* name) {
 }
 // (an output's rows must not lie over one another)
 void apart(const at::Tensor& t, const char* name) {
-  for (int i = 0; i < t.dim(); ++i) need(t.size(i) < 2 || t.stride(i) != 0, std::string(name) + ": an output must not be expanded");
+  for (int i = 0; i < t.dim(); ++i) NEED(t.size(i) < 2 || t.stride(i) != 0, std::string(name) + ": an output must not be expanded");
 }
 
 tsd_paged_cache cache_of(const at::Tensor& k, const at::Tensor& v, const at::Tensor& table, int64_t B) {
   tsd_paged_cache c;
   c.dtype = dtype_of(k, "k_pool");
   on_gpu(k, "k_pool");
-  need(k.dim() == 4, "k_pool must be [pages, page_tokens, kv_heads, head_dim]");
+  NEED(k.dim() == 4, "k_pool must be [pages, page_tokens, kv_heads, head_dim]");
   like(v, k, "v_pool");
-  need(v.sizes() == k.sizes() && v.strides() == k.strides(), "k_pool and v_pool must have the same shape and strides");
-  need(k.numel() > 0 && k.stride(3) == 1, "k_pool: needs a page, and heads that are dense");
-  need(table.device() == k.device() && table.scalar_type() == at::kInt, "page_table must be int32, on the pools' device");
-  need(table.dim() == 2 && table.size(0) == B && table.size(1) > 0 && (table.stride(1) == 1 || table.size(1) == 1),
+  NEED(v.sizes() == k.sizes() && v.strides() == k.strides(), "k_pool and v_pool must have the same shape and strides");
+  NEED(k.numel() > 0 && k.stride(3) == 1, "k_pool: needs a page, and heads that are dense");
+  NEED(table.device() == k.device() && table.scalar_type() == at::kInt, "page_table must be int32, on the pools' device");
+  NEED(table.dim() == 2 && table.size(0) == B && table.size(1) > 0 && (table.stride(1) == 1 || table.size(1) == 1),
        "page_table must be [B, pages per sequence], rows dense");
   c.k_dev = k.data_ptr();
   c.v_dev = v.data_ptr();
@@ -212,7 +214,7 @@ tsd_paged_cache cache_of(const at::Tensor& k, const at::Tensor& v, const at::Ten
   c.head_stride = k.size(2) > 1 ? k.stride(2) : 0;
   c.page_table_dev = static_cast<const int32_t*>(table.data_ptr());
   c.pages_per_seq = whole(table.size(1), "page_table");
-  need(B < 2 || table.stride(0) >= table.size(1), "page_table: rows must not overlap");
+  NEED(B < 2 || table.stride(0) >= table.size(1), "page_table: rows must not overlap");
   c.table_stride = B > 1 ? whole(table.stride(0), "page_table") : c.pages_per_seq;
   c.n_pages = whole(k.size(0), "k_pool");
   c.page_tokens = whole(k.size(1), "k_pool");
@@ -246,7 +248,7 @@ PyObject* rope_append_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int inter = PyObject_IsTrue(args[10]);
     const double amplitude = PyFloat_AsDouble(args[11]);
     if (PyErr_Occurred()) return nullptr;
-    need(q.dim() == 4, "q must be [B, T, heads, head_dim]");
+    NEED(q.dim() == 4, "q must be [B, T, heads, head_dim]");
     const int64_t B = q.size(0), T = q.size(1);
     tsd_paged_cache cache = cache_of(k_pool, v_pool, table, B);
     like(q, k_pool, "q");
@@ -258,7 +260,7 @@ PyObject* rope_append_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     plain(base, q, at::kInt, {B}, "base");
     if (positions) plain(*positions, q, at::kInt, {B, T}, "positions");
     if (n_new) plain(*n_new, q, at::kInt, {B}, "n_new");
-    need(freq.dim() == 1, "freq must be [rotary_dim / 2]");
+    NEED(freq.dim() == 1, "freq must be [rotary_dim / 2]");
     plain(freq, q, at::kDouble, {freq.size(0)}, "freq");
     const c10::DeviceGuard guard(q.device());
     at::Tensor out = to ? *to : at::empty({B, T, q.size(2), cache.head_dim}, q.options());
@@ -290,7 +292,7 @@ PyObject* paged_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor *n_new = maybe(args[7], "n_new"), *to = maybe(args[8], "out");
     const int want_lse = PyObject_IsTrue(args[9]);
     if (PyErr_Occurred()) return nullptr;
-    need(q.dim() == 4, "q must be [B, T, heads, head_dim]");
+    NEED(q.dim() == 4, "q must be [B, T, heads, head_dim]");
     const int64_t B = q.size(0), T = q.size(1), H = q.size(2);
     tsd_paged_cache cache = cache_of(k_pool, v_pool, table, B);
     like(q, k_pool, "q");
@@ -333,14 +335,14 @@ PyObject* verify_tokens_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor* n_draft = maybe(args[4], "n_draft");
     on_gpu(p, "p");
     const int dtype = dtype_of(p, "p");
-    need(draft.dim() == 2 && p.dim() == 3, "draft must be [B, K], p [B, K + 1, V]");
-    need(draft.scalar_type() == at::kInt || draft.scalar_type() == at::kLong, "draft must be int32 or int64");
+    NEED(draft.dim() == 2 && p.dim() == 3, "draft must be [B, K], p [B, K + 1, V]");
+    NEED(draft.scalar_type() == at::kInt || draft.scalar_type() == at::kLong, "draft must be int32 or int64");
     const int64_t B = draft.size(0), K = draft.size(1), V = p.size(2);
     plain(draft, p, draft.scalar_type(), {B, K}, "draft");
-    need(p.size(0) == B && p.size(1) == K + 1 && (V == 1 || p.stride(2) == 1), "p must be [B, K + 1, V], rows dense");
+    NEED(p.size(0) == B && p.size(1) == K + 1 && (V == 1 || p.stride(2) == 1), "p must be [B, K + 1, V], rows dense");
     if (q) {
       like(*q, p, "q");
-      need(q->dim() == 3 && q->size(0) == B && q->size(1) == K && q->size(2) == V && (V == 1 || q->stride(2) == 1), "q must be [B, K, V], rows dense");
+      NEED(q->dim() == 3 && q->size(0) == B && q->size(1) == K && q->size(2) == V && (V == 1 || q->stride(2) == 1), "q must be [B, K, V], rows dense");
     }
     plain(uniforms, p, at::kFloat, {B, K + 1}, "uniforms");
     if (n_draft) plain(*n_draft, p, at::kInt, {B}, "n_draft");
