@@ -9,6 +9,7 @@
 #pragma once
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "tsd_internal.h"
 
@@ -22,11 +23,16 @@ inline uint64_t new_tag() {
 }
 
 #if defined(__HIPCC__)
-__device__ __forceinline__ void leave(double* to, double v) {
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// (V: 4 or 8 bytes)
+template <typename V>
+using WordOf = std::conditional_t<sizeof(V) == 8, uint64_t, uint32_t>;
+template <typename V>
+__device__ __forceinline__ void leave(V* to, V v) {
+  __hip_atomic_store(reinterpret_cast<WordOf<V>*>(to), __builtin_bit_cast(WordOf<V>, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ double left_by_all(const double* from) {
-  return __builtin_bit_cast(double, __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+template <typename V>
+__device__ __forceinline__ V left(const V* from) {
+  return __builtin_bit_cast(V, __hip_atomic_load(reinterpret_cast<const WordOf<V>*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
 // For a whole workgroup, once it has left its part: whether it finishes the group of `n`, whose slot `own` is its.

@@ -5,8 +5,10 @@
 //
 // Split: the keys of a sequence go in chunks of `chunk`; a workgroup takes one (sequence, key head, row tile, chunk), its wavefronts take
 // its steps of 32 keys in turn, each with a running maximum and sum of its own, joined in LDS at the end.  Where a sequence may
-// have several chunks, each leaves its rows' normalised sums and their logarithm (base 2) in the workspace, and a second launch joins those.
+// have several chunks, each leaves its rows' normalised sums and their logarithm (base 2) in the workspace.  They are joined by the workgroup
+// of a (sequence, key head, row tile) that comes last (last_arriver.h), or, where that is much for one workgroup, by a second launch.
 #pragma once
+#include "last_arriver.h"
 #include "paged_cache.h"
 
 namespace tsd {
@@ -22,6 +24,8 @@ struct PagedAttnP {
   float scale2;      // scale * log2(e)
   float* part_o;     // [B][splits][T][Hq][D] (splits > 1)
   float* part_lse;   // [B][splits][T][Hq]
+  uint64_t* slots;   // [B][Hkv][row_tiles][splits], or NULL: a second launch joins
+  uint64_t tag;
 };
 
 constexpr int kAttnWaves = 4;  // most wavefronts a workgroup has
@@ -144,6 +148,17 @@ __device__ __forceinline__ float attn_taken(float v) { return (__float_as_uint(v
 // The first key of the mixed steps of `step` keys.
 __device__ __forceinline__ int attn_mixed_from(const AttnWork& w, int step) { return w.key0 + max(w.see_first - w.key0, 0) / step * step; }
 
+// Writes dims d .. d + 3 of a row of the output.
+template <typename T>
+__device__ __forceinline__ void attn_write(const PagedAttnP& p, int b, int t, int h, int d, f32x4 o, float inv, float lse2) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 y;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = (T)(o[j] * inv);
+  *reinterpret_cast<T4*>(reinterpret_cast<T*>(p.out.p) + b * p.out.sb + t * p.out.st + h * p.out.sh + d) = y;
+  if (d == 0 && p.lse) p.lse[((long)b * p.T + t) * p.Hq + h] = lse2 * 0.69314718055994531f;
+}
+
 // Writes dims d .. d + 3 of a row's sums, times inv: to the output, or to the workspace where a sequence may have several chunks.
 template <typename T>
 __device__ __forceinline__ void attn_store(const PagedAttnP& p, const AttnWork& w, int row, int d, f32x4 o, float inv, float lse2) {
@@ -152,16 +167,80 @@ __device__ __forceinline__ void attn_store(const PagedAttnP& p, const AttnWork& 
     const long r = (((long)w.b * p.splits + w.split) * p.T + t) * p.Hq + h;
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] *= inv;
-    *reinterpret_cast<f32x4*>(p.part_o + r * p.D + d) = o;
-    if (d == 0) p.part_lse[r] = lse2;
+    f32x4* to = reinterpret_cast<f32x4*>(p.part_o + r * p.D + d);
+    if (p.slots) {
+      leave(reinterpret_cast<float2*>(to), make_float2(o[0], o[1]));
+      leave(reinterpret_cast<float2*>(to) + 1, make_float2(o[2], o[3]));
+      if (d == 0) leave(p.part_lse + r, lse2);
+    } else {
+      *to = o;
+      if (d == 0) p.part_lse[r] = lse2;
+    }
   } else {
-    typedef T T4 __attribute__((ext_vector_type(4)));
-    T4 y;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = (T)(o[j] * inv);
-    *reinterpret_cast<T4*>(reinterpret_cast<T*>(p.out.p) + w.b * p.out.sb + t * p.out.st + h * p.out.sh + d) = y;
-    if (d == 0 && p.lse) p.lse[((long)w.b * p.T + t) * p.Hq + h] = lse2 * 0.69314718055994531f;
+    attn_write<T>(p, w.b, t, h, d, o, inv, lse2);
   }
+}
+
+// Sums of a row's chunks, as they come: o and sum relative to 2^m.
+struct AttnJoin {
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f, m = -INFINITY;
+  __device__ __forceinline__ void add(float lse2, f32x4 y) {
+    if (lse2 == -INFINITY) return;  // (a chunk without keys of this row)
+    const float top = fmaxf(m, lse2), a = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(lse2 - top);
+    sum = sum * a + f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = o[j] * a + f * y[j];
+    m = top;
+  }
+};
+
+// The end of a workgroup of a split call: if it came last of its (sequence, key head, row tile), it joins the chunks.  A lane takes 4 dims of a
+// row; where that leaves lanes idle, groups of lanes take every so many chunks.  buf: float [blockDim.x][6] in LDS.
+template <typename T>
+__device__ __forceinline__ void attn_finish(const PagedAttnP& p, const AttnWork& w, int tile_rows, float* buf) {
+  const int chunks = attn_chunks(p, w.len);
+  uint64_t* slots = p.slots + (((long)w.b * p.Hkv + w.hk) * p.row_tiles + w.tile) * p.splits;
+  if (!came_last(slots, chunks, w.split, p.tag)) return;
+  const int lpr = p.D / 4, items = min(w.rows - w.row0, tile_rows) * lpr;
+  const int groups = max(1, min((int)blockDim.x / items, chunks)), grp = groups > 1 ? threadIdx.x / items : 0;
+  const long step = (long)p.T * p.Hq;
+  for (int i = groups > 1 ? threadIdx.x - grp * items : threadIdx.x; i < items; i += blockDim.x) {
+    const int lr = i / lpr, d = (i - lr * lpr) * 4, row = w.row0 + lr, t = row / p.G, h = w.hk * p.G + row - t * p.G;
+    const long r = ((long)w.b * p.splits * p.T + t) * p.Hq + h;
+    AttnJoin join;
+    constexpr int U = 8;  // chunks whose loads are on their way together
+    if (grp < groups)
+      for (int s0 = grp; s0 < chunks; s0 += U * groups) {
+        float l[U];
+        float2 y[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const long at = r + min(s0 + u * groups, chunks - 1) * step;
+          l[u] = left(p.part_lse + at);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) y[u][j] = left(reinterpret_cast<const float2*>(p.part_o + at * p.D + d) + j);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (s0 + u * groups < chunks) join.add(l[u], f32x4{y[u][0].x, y[u][0].y, y[u][1].x, y[u][1].y});
+      }
+    if (groups > 1) {  // (then every lane is here once)
+      float* own = buf + threadIdx.x * 6;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) own[j] = join.sum == 0.f ? 0.f : join.o[j] / join.sum;
+      own[4] = join.sum == 0.f ? -INFINITY : join.m + __builtin_amdgcn_logf(join.sum);
+      __syncthreads();
+      if (grp) break;
+      for (int v = 1; v < groups; ++v) {
+        const float* x = buf + (threadIdx.x + v * items) * 6;
+        join.add(x[4], f32x4{x[0], x[1], x[2], x[3]});
+      }
+    }
+    const bool none = join.sum == 0.f;
+    attn_write<T>(p, w.b, t, h, d, join.o, none ? 0.f : 1.f / join.sum, none ? -INFINITY : join.m + __builtin_amdgcn_logf(join.sum));
+  }
+  clear_slots(slots, chunks);
 }
 
 // Joins the wavefronts' sums of one tile of 16 rows through LDS and writes them.  O: this wavefront's sums of row `lr`, written by put(row, buf_row);

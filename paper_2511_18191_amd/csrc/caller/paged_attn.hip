@@ -211,6 +211,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
         for (int r = 0; r < 4; ++r) to[(4 * g + r) * rs + nb * 16 + qi] = o[mt][nb][r];
     });
   }
+  if (p.slots) attn_finish<bf16>(p, w, 16 * MT, reinterpret_cast<float*>(smem));
 }
 
 // Joins the chunks of a row: WPR wavefronts take one, their lanes 4 dims each, as many groups of lanes as a wavefront has room for
@@ -268,12 +269,7 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(const PagedAttnP p
     }
   const bool none = sum == 0.f;
   const float inv = none ? 0.f : 1.f / sum;
-  typedef T T4 __attribute__((ext_vector_type(4)));
-  T4 y;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) y[j] = (T)(o[j] * inv);
-  *reinterpret_cast<T4*>(reinterpret_cast<T*>(p.out.p) + b * p.out.sb + t * p.out.st + h * p.out.sh + d) = y;
-  if (d == 0 && p.lse) p.lse[((long)b * p.T + t) * p.Hq + h] = none ? -INFINITY : (mm + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+  attn_write<T>(p, b, t, h, d, o, inv, none ? -INFINITY : mm + __builtin_amdgcn_logf(sum));
 }
 
 template <typename T>
@@ -300,9 +296,19 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 }
 
 // What the sizes make of a call.
+//
+// Chunks: as many as give every compute unit one workgroup (256 in all: a step more and some get two, 32 x 1 x 1024 keys of 8 heads 33.7 us,
+// 36 x 896 42.9), none shorter than a step of all wavefronts, and of at most 1024 keys where up to four workgroups a compute unit would
+// otherwise go by the longest sequence (64 ragged sequences of up to 8192: whole 239 us, 1024 keys 217, 256 keys 256).  With more
+// workgroups than that, sequences stay whole.  At most 16384 workgroups, most of them idle, where max_len says much more than lengths are.
+// Joins: by the last workgroup where that is little work for one (12 chunks of 9 rows of 80: 17.5 us against 19.0 with a second launch, 8 of 8 rows of
+// 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3).
+// Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys
+// 45.9 us, two 46.8, four 52.0).
 struct AttnPlan {
   bool prompt;  // the kernel for many rows
   int mt, waves, row_tiles, splits, chunk;
+  bool joins;   // the last workgroup of a tile joins its chunks
 };
 
 AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len) {
@@ -312,16 +318,20 @@ AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len)
   a.mt = rows <= 16 || D > 128 ? 1 : 2;
   const int tile_rows = a.prompt ? kPromptRows : 16 * a.mt;
   a.row_tiles = (rows + tile_rows - 1) / tile_rows;
-  const int64_t base = (int64_t)B * Hkv * a.row_tiles, steps = (max_len + 31) / 32;
+  const int64_t base = (int64_t)B * Hkv * a.row_tiles, steps = (max_len + 31) / 32;  // workgroups where nothing is split
   a.waves = a.prompt ? kPromptWaves : (int)std::min<int64_t>(base >= 1024 && steps <= 4 ? 1 : D > 128 ? 2 : kAttnWaves, steps);
   const int64_t step = a.prompt ? 64 : 32 * a.waves;
   int64_t chunk = max_len;
-  if (a.prompt ? base < 256 : base < 1024) chunk = std::min<int64_t>(max_len * base / 256 / step * step, a.prompt ? max_len : 1024);
+  if (a.prompt ? base < 256 : base < 1024) {
+    chunk = std::min<int64_t>(max_len * base / 256, a.prompt ? max_len : 1024);
+    chunk = chunk < step + step / 4 ? step : (chunk + step - 1) / step * step;
+  }
   if (a.prompt) chunk = std::max<int64_t>(chunk, 512);
   chunk = std::max(chunk, max_len * base / 16384);
   chunk = std::max(step, (chunk + step - 1) / step * step);
   a.chunk = (int)chunk;
   a.splits = (max_len + a.chunk - 1) / a.chunk;
+  a.joins = a.splits > 1 && a.splits <= 16 && base < 256 && a.splits * std::min(rows, tile_rows) * D <= 16384;
   return a;
 }
 
@@ -336,10 +346,11 @@ int check_attn(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_h
   return TSD_OK;
 }
 
-size_t attn_bytes(const AttnPlan& a, int B, int T, int Hq, int D) {
+// The workspace: sums, logarithms, slots.
+size_t attn_part_bytes(const AttnPlan& a, int B, int T, int Hq, int D) { return ((size_t)B * a.splits * T * Hq * (D + 1) * 4 + 7) / 8 * 8; }
+size_t attn_bytes(const AttnPlan& a, int B, int T, int Hq, int Hkv, int D) {
   if (a.splits == 1) return 0;
-  const size_t rows = (size_t)B * a.splits * T * Hq;
-  return (rows * D * 4 + rows * 4 + 255) / 256 * 256;
+  return (attn_part_bytes(a, B, T, Hq, D) + (size_t)B * Hkv * a.row_tiles * a.splits * 8 + 255) / 256 * 256;
 }
 
 }  // namespace
@@ -359,7 +370,7 @@ extern "C" int tsd_paged_attn_workspace(const tsd_paged_cache* cache, int32_t B,
   const int rc = check_attn(cache, B, T, n_q_heads, max_len);
   if (rc) return rc;
   if (!bytes_host) return fail_no_handle(TSD_E_INVALID_ARG, "bytes_host must not be NULL");
-  *bytes_host = attn_bytes(attn_plan(cache->dtype, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim, max_len), B, T, n_q_heads, cache->head_dim);
+  *bytes_host = attn_bytes(attn_plan(cache->dtype, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim, max_len), B, T, n_q_heads, cache->n_kv_heads, cache->head_dim);
   return TSD_OK;
 }
 
@@ -373,7 +384,7 @@ extern "C" int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, in
   if (!lens_dev) return fail_no_handle(TSD_E_INVALID_ARG, "lens_dev must not be NULL");
   if (!std::isfinite(scale)) return fail_no_handle(TSD_E_INVALID_ARG, "scale must be finite");
   const AttnPlan a = attn_plan(cache->dtype, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim, max_len);
-  const size_t need = attn_bytes(a, B, T, n_q_heads, cache->head_dim);
+  const size_t need = attn_bytes(a, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim);
   if (need && (!workspace_dev || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
     return fail_no_handle(TSD_E_INVALID_ARG, "workspace: needs the bytes that tsd_paged_attn_workspace gives for these sizes, 16-byte aligned");
   if ((int64_t)B * cache->n_kv_heads * a.row_tiles * a.splits > INT32_MAX) return fail_no_handle(TSD_E_OUT_OF_RANGE, "more than 2^31 workgroups");
@@ -396,10 +407,12 @@ extern "C" int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, in
   p.scale2 = scale * 1.44269504088896341f;
   p.part_o = static_cast<float*>(workspace_dev);
   p.part_lse = need ? p.part_o + (size_t)B * a.splits * T * n_q_heads * cache->head_dim : nullptr;
+  p.slots = a.joins ? reinterpret_cast<uint64_t*>(static_cast<char*>(workspace_dev) + attn_part_bytes(a, B, T, n_q_heads, cache->head_dim)) : nullptr;
+  p.tag = a.joins ? new_tag() : 0;
   const hipStream_t st = (hipStream_t)stream;
   hipError_t e = a.prompt                   ? launch_paged_attn_prompt(p, st)
                  : cache->dtype == TSD_BF16 ? launch_paged_attn_bf16(p, a.mt, a.waves, st)
                                             : launch_paged_attn_f32(p, a.mt, a.waves, st);
-  if (e == hipSuccess && a.splits > 1) e = cache->dtype == TSD_BF16 ? launch_join<bf16>(p, st) : launch_join<float>(p, st);
+  if (e == hipSuccess && a.splits > 1 && !a.joins) e = cache->dtype == TSD_BF16 ? launch_join<bf16>(p, st) : launch_join<float>(p, st);
   return e == hipSuccess ? TSD_OK : fail_no_handle(TSD_E_HIP, std::string("paged attention launch: ") + hipGetErrorString(e));
 }

@@ -192,6 +192,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
         }
     });
   }
+  if (p.slots) attn_finish<float>(p, w, 16 * MT, reinterpret_cast<float*>(smem));
 }
 
 template <int DP>

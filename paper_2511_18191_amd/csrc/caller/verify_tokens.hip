@@ -177,7 +177,7 @@ template <bool ONE>
 __device__ __forceinline__ Found find_segment(const double* sums, int segments, double u) {
   const int lane = threadIdx.x & 63, per = (segments + 63) / 64, first = lane * per, last = min(segments, first + per);
   double own = 0.0;
-  const auto sum = [&](int s) { return ONE ? sums[s] : left_by_all(sums + s); };
+  const auto sum = [&](int s) { return ONE ? sums[s] : left(sums + s); };
   for (int s = first; s < last; ++s) own += sum(s);
   const double upto = wave_scan(own);
   const double whole = __shfl(upto, 63), prev = __shfl_up(upto, 1);
