@@ -105,6 +105,10 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
     const bool more = sb + stride < w.key1;
     next_valid = (unsigned)__ballot(off >= 0);
     off = max(off, 0l);
+    // (the entries of the step after the next are read before loads are issued that nothing waits for yet: counted waits do not
+    // survive the branches between)
+    const long later = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
+    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
     const bool whole = valid == 0xFFFFFFFFu && sb + 32 <= w.see_first;  // every row of the tile sees every key
     if (!whole) {
       // keys that are not there hold anything; their weights are 0, and so must the values be
@@ -134,8 +138,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
         for (int kk = 0; kk < KK; ++kk) sc[mt][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[bi][kk], qf[mt][kk], sc[mt][bi], 0, 0, 0);
       }
     if (more) load_k(off);
-    off = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
-    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
+    off = later;
 
     bf16x8 pf[MT];
 #pragma unroll
@@ -301,6 +304,9 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // 36 x 896 42.9), none shorter than a step of all wavefronts, and of at most 1024 keys where up to four workgroups a compute unit would
 // otherwise go by the longest sequence (64 ragged sequences of up to 8192: whole 239 us, 1024 keys 217, 256 keys 256).  With more
 // workgroups than that, sequences stay whole.  At most 16384 workgroups, most of them idle, where max_len says much more than lengths are.
+// Kernel: the one for many rows from 65 rows a key head on (68 of 128, us for 64 sequences of up to 8192: 296 against 622; 120 of 80, 32 of up to 2000:
+// 51 against 67), and from 33 on where heads are wide and workgroups enough (40 of 128, 64 sequences: 278 against 435, 8: 45 against 51; but
+// 36 of 64, 128 sequences of up to 2000: 74 against 62).
 // Joins: by the last workgroup where that is little work for one (12 chunks of 9 rows of 80: 17.5 us against 19.0 with a second launch, 8 of 8 rows of
 // 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3).
 // Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys
@@ -314,7 +320,7 @@ struct AttnPlan {
 AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len) {
   AttnPlan a;
   const int rows = T * (Hq / Hkv);
-  a.prompt = dtype == TSD_BF16 && D <= 128 && rows > 64;
+  a.prompt = dtype == TSD_BF16 && D <= 128 && (rows > 64 || (rows > 32 && D > 96 && (int64_t)B * Hkv >= 64));
   a.mt = rows <= 16 || D > 128 ? 1 : 2;
   const int tile_rows = a.prompt ? kPromptRows : 16 * a.mt;
   a.row_tiles = (rows + tile_rows - 1) / tile_rows;
@@ -322,11 +328,12 @@ AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len)
   a.waves = a.prompt ? kPromptWaves : (int)std::min<int64_t>(base >= 1024 && steps <= 4 ? 1 : D > 128 ? 2 : kAttnWaves, steps);
   const int64_t step = a.prompt ? 64 : 32 * a.waves;
   int64_t chunk = max_len;
-  if (a.prompt ? base < 256 : base < 1024) {
-    chunk = std::min<int64_t>(max_len * base / 256, a.prompt ? max_len : 1024);
+  const bool tall = a.prompt && a.row_tiles > 1;  // (sums of many rows cost more to join than unequal lengths do)
+  if (base < (tall ? 256 : 1024)) {
+    chunk = std::min<int64_t>(max_len * base / 256, tall ? max_len : 1024);
     chunk = chunk < step + step / 4 ? step : (chunk + step - 1) / step * step;
   }
-  if (a.prompt) chunk = std::max<int64_t>(chunk, 512);
+  if (a.prompt) chunk = std::max<int64_t>(chunk, 256);
   chunk = std::max(chunk, max_len * base / 16384);
   chunk = std::max(step, (chunk + step - 1) / step * step);
   a.chunk = (int)chunk;

@@ -88,6 +88,10 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
     const bool more = sb + stride < w.key1;
     next_valid = (unsigned)__ballot(off >= 0);
     off = max(off, 0l);
+    // (the entries of the step after the next are read before loads are issued that nothing waits for yet: counted waits do not
+    // survive the branches between)
+    const long later = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
+    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
     const bool whole = valid == 0xFFFFFFFFu && sb + 32 <= w.see_first;
     f32x4 sc[MT][2];
 #pragma unroll
@@ -151,8 +155,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
             for (int mt = 0; mt < MT; ++mt)
               o[mt][c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(e[mt][4 * bi + r], vf[bi][r][c][j], o[mt][c][j], 0, 0, 0);
     if (more) load_v(off);
-    off = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
-    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
+    off = later;
   }
 
   if (__any(odd)) {

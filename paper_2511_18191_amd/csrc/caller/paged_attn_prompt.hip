@@ -1,19 +1,23 @@
 // tsd_paged_attn_static on bf16 caches, many rows: chunks of prompts.
 //
-// Operations bound these calls, so keys and values are staged in LDS once for all rows of a workgroup (64 a wavefront), and both products run on
+// Operations bound these calls, so keys and values are staged in LDS once for all rows of a workgroup (32 a wavefront), and both products run on
 // 32x32x16 matrix instructions with the rows along the lanes:
 //   S^T = K Q^T    lane (row r = lane % 32, half h = lane / 32) ends up with keys 8 i + 4 h + j (i, j < 4) of each 32;
 //   O^T += V^T P^T the contraction's order is free, so those same keys are its operand as they lie, and V rows are picked up transposed for
 //                  them (ds_read_b64_tr_b16: 4 keys of one dim).
 // Maximum, sum and rescaling of a row stay in its two lanes: one exchange between the halves per 64 keys, and nothing crosses lanes for the
-// sums.  64 rows a wavefront because a wavefront reads all of a tile from LDS: at 32 rows that read (16 KB per 32 keys, 128 B a clock) takes
-// as long as the matrix instructions it feeds.
+// sums.  The weights are rounded to bf16, the instruction's operand; their sum is not.
+// 32 rows a wavefront at 252 registers, two on a SIMD: one forms weights while the other multiplies.  (64 rows would read LDS half as often, but
+// do not fit: 350 registers and spills.)
+// 2 x 1024 tokens behind 2048, 32 heads over 8 of 128: 110 us, 0.78 PFLOP/s; weights and products overlap only in part, and both take some
+// 1000 clocks per 64 keys and 32 rows.
 #include "paged_attn.h"
 
 namespace tsd {
 namespace {
 
 constexpr int kTile = 64;      // keys a tile
+constexpr float kLag = 6.f;    // weights up to 64: bf16's steps and fp32's sums are as fine there
 
 // 16-byte chunk `c` of row `r` lies at chunk c ^ turn(r) of its row: one chunk of 16 rows, and four of 4, cover all 256 bytes of the banks.
 template <int DP>
@@ -21,10 +25,10 @@ __device__ __forceinline__ int turn(int r) {
   return DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
 }
 
-template <int DP, int WAVES, int CT, bool FULL>  // FULL: head_dim is DP
+template <int DP, int WAVES, bool FULL>  // FULL: head_dim is DP
 __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  constexpr int kWaveRows = 32 * CT, KK = DP / 16, DB = DP / 32, CPR = DP / 8, THREADS = WAVES * 64, NL = kTile * CPR / THREADS;
+  constexpr int kWaveRows = 32, KK = DP / 16, DB = DP / 32, CPR = DP / 8, THREADS = WAVES * 64, NL = kTile * CPR / THREADS;
   AttnWork w = attn_place(p, WAVES * kWaveRows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r32 = lane & 31, h = lane >> 5;
   const int* table = p.cache.table + (long)w.b * p.cache.table_stride;
@@ -38,39 +42,41 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
   const float scale2 = fmaxf(fabsf(p.scale2), 1.2e-38f);
 
   const int row0 = w.row0 + wave * kWaveRows;
-  bf16x8 qf[CT][KK];
-  int sees[CT];
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int row = row0 + ct * 32 + r32;
-    sees[ct] = attn_sees(p, w, row);
+  const int row = row0 + r32, sees = attn_sees(p, w, row);
+  bf16x8 qf[KK];
+  {
     const int r = min(row, w.rows - 1), t = r / p.G, hq = w.hk * p.G + r - t * p.G;
     const bf16* q = reinterpret_cast<const bf16*>(p.q.p) + w.b * p.q.sb + t * p.q.st + hq * p.q.sh;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       const int d = kk * 16 + h * 8;
-      qf[ct][kk] = FULL || d < p.D ? *reinterpret_cast<const bf16x8*>(q + d) : zero;
-      if (p.scale2 < 0.f) qf[ct][kk] = -qf[ct][kk];
+      qf[kk] = FULL || d < p.D ? *reinterpret_cast<const bf16x8*>(q + d) : zero;
+      if (p.scale2 < 0.f) qf[kk] = -qf[kk];
     }
   }
-  // keys that the wavefront's first and last rows see
+  // keys that the wavefront's first and last rows see (a wavefront without rows only loads)
   const int see_first = row0 + kWaveRows <= w.rows ? attn_sees(p, w, row0) : 0;
-  const int see_last = attn_sees(p, w, min(row0 + kWaveRows, w.rows) - 1);
+  const int see_last = row0 < w.rows ? attn_sees(p, w, min(row0 + kWaveRows, w.rows) - 1) : 0;
 
-  f32x16 o[CT][DB];
-  float m_run[CT], l_run[CT];
+  f32x16 o[DB];
+  float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    m_run[ct] = -INFINITY;
-    l_run[ct] = 0.f;
+  for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[ct][db][i] = 0.f;
-  }
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
 
   bf16x8 kr[NL], vr[NL];
-  auto load = [&](long off) {
+  auto load = [&](long off, unsigned long long there) {
+    if (FULL && there == ~0ull) {  // (nearly always: no lane has to be kept from its load)
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int c = i * THREADS + threadIdx.x;
+        const long o_r = __shfl(off, c / CPR) + (c % CPR) * 8;
+        kr[i] = *reinterpret_cast<const bf16x8*>(kbase + o_r);
+        vr[i] = *reinterpret_cast<const bf16x8*>(vbase + o_r);
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int c = i * THREADS + threadIdx.x, r = c / CPR, d = (c % CPR) * 8;
@@ -83,7 +89,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
   long off = attn_key_row(p, w, entry, w.key0 + lane);
   entry = next_entry;
   unsigned long long valid = __ballot(off >= 0), next_valid = 0;
-  if (w.key0 < w.key1) load(off);
+  if (w.key0 < w.key1) load(off, valid);
   off = attn_key_row(p, w, entry, w.key0 + kTile + lane);
   entry = paged_entry(p.cache, table, w.key0 + 2 * kTile + lane);
   int parity = 0;
@@ -105,71 +111,69 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
     }
     // (two buffers: who writes one has left it a barrier ago)
     __syncthreads();
-    if (sb + kTile < w.key1) load(off);
-    off = attn_key_row(p, w, entry, sb + 2 * kTile + lane);
+    // (the entries of the tile after the next are read before loads are issued that nothing waits for yet: counted waits do not
+    // survive the branches between)
+    const long later = attn_key_row(p, w, entry, sb + 2 * kTile + lane);
     entry = paged_entry(p.cache, table, sb + 3 * kTile + lane);
+    if (sb + kTile < w.key1) load(off, next_valid);
+    off = later;
     if (sb >= see_last) continue;
 
-    f32x16 sc[2][CT];  // [32 keys][column block]
+    f32x16 sc[2];  // of 32 keys each
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[s][ct][i] = 0.f;
+      for (int i = 0; i < 16; ++i) sc[s][i] = 0.f;
       const int r = s * 32 + r32;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
         const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + r * DP + ((2 * kk + h) ^ turn<DP>(r)) * 8);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) sc[s][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ct][kk], sc[s][ct], 0, 0, 0);
+        sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], sc[s], 0, 0, 0);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
     const bool whole = valid == ~0ull && sb + kTile <= see_first;
-    bf16x8 pf[CT][2][2];  // [column block][32 keys][16 of them]
+    if (!whole) {
+      const int left = sees - sb - 4 * h;  // (the lane's keys are 4 h further on than these)
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      if (!whole) {
-        const int left = sees[ct] - sb - 4 * h;  // (the lane's keys are 4 h further on than these)
+      for (int s = 0; s < 2; ++s) {
+        const unsigned there = (unsigned)(valid >> (4 * h) >> (32 * s));
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const unsigned there = (unsigned)(valid >> (4 * h) >> (32 * s));
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!(there >> (8 * (i >> 2) + (i & 3)) & 1) || s * 32 + 8 * (i >> 2) + (i & 3) >= left) sc[s][ct][i] = -INFINITY;
-        }
-      }
-      // (maxima are those of the products; a negative factor has gone into the queries, and one of 0 is too small to tell scores apart)
-      float mx = sc[0][ct][0];
-#pragma unroll
-      for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][ct][i & 15]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float m_new = fmaxf(m_run[ct], mx);
-      const float shift = m_new == -INFINITY ? 0.f : -m_new * scale2;
-      const float alpha = __builtin_amdgcn_exp2f(fmaf(m_run[ct], scale2, shift));
-      m_run[ct] = m_new;
-      float sum = 0.f;
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(sc[s][ct][i], scale2, shift));
-          sum += e;
-          pf[ct][s][i >> 3][i & 7] = (bf16)e;
-        }
-      l_run[ct] = l_run[ct] * alpha + sum;
-      if (__any(alpha != 1.f)) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[ct][db][i] *= alpha;
+        for (int i = 0; i < 16; ++i)
+          if (!(there >> (8 * (i >> 2) + (i & 3)) & 1) || s * 32 + 8 * (i >> 2) + (i & 3) >= left) sc[s][i] = -INFINITY;
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    // operand of the values: keys 16 m + 8 (j / 4) + 4 h + j % 4, j = 0 .. 7, of each 32, for dim lane % 32 of a block
+    // (maxima are those of the products; a negative factor has gone into the queries, and one of 0 is too small to tell scores apart)
+    float mx = sc[0][0];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    // Sums are kept relative to a maximum that may lag by a factor of 2^kLag: most tiles raise some row's by a little, and leave the sums alone.
+    const bool raise = (mx - m_run) * scale2 > kLag;  // (the first key a row sees, too)
+    if (__any(raise)) {
+      float alpha = 1.f;
+      if (raise) {
+        alpha = __builtin_amdgcn_exp2f((m_run - mx) * scale2);
+        m_run = mx;
+      }
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
+    const float shift = m_run == -INFINITY ? 0.f : -m_run * scale2;
+    // 32 keys' weights, then their product with the values: the matrix cores run behind while the next weights are formed
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      bf16x8 pf[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(sc[s][i], scale2, shift));
+        l_run += e;
+        pf[i >> 3][i & 7] = (bf16)e;
+      }
+      // operand of the values: keys 16 m + 8 (j / 4) + 4 h + j % 4, j = 0 .. 7, for dim lane % 32 of a block
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -184,9 +188,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
             hv[part] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)src);
           }
           const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(hv[0], hv[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) o[ct][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf[ct][s][m], o[ct][db], 0, 0, 0);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf[m], o[db], 0, 0, 0);
         }
+    }
   }
   if (__syncthreads_or(odd)) {
     for (int key = attn_mixed_from(w, kTile); key < w.key1; ++key) {
@@ -199,26 +203,21 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
         if (FULL || d < p.D) v = *reinterpret_cast<const bf16x4*>(vbase + at + d);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-            if (key < sees[ct]) o[ct][i >> 2][(i & 3) * 4 + j] += attn_taken((float)v[j]);
+          if (key < sees) o[i >> 2][(i & 3) * 4 + j] += attn_taken((float)v[j]);
       }
     }
   }
 
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const float sum = l_run[ct] + __shfl_xor(l_run[ct], 32);
-    const int row = row0 + ct * 32 + r32;
-    if (row >= w.rows) continue;
+  const float sum = l_run + __shfl_xor(l_run, 32);
+  if (row < w.rows) {
     const bool none = sum == 0.f;
-    const float inv = none ? 0.f : 1.f / sum, lse2 = none ? -INFINITY : m_run[ct] * scale2 + __builtin_amdgcn_logf(sum);
+    const float inv = none ? 0.f : 1.f / sum, lse2 = none ? -INFINITY : m_run * scale2 + __builtin_amdgcn_logf(sum);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int d = db * 32 + 8 * i + 4 * h;
-        if (FULL || d < p.D) attn_store<bf16>(p, w, row, d, f32x4{o[ct][db][4 * i], o[ct][db][4 * i + 1], o[ct][db][4 * i + 2], o[ct][db][4 * i + 3]}, inv, lse2);
+        if (FULL || d < p.D) attn_store<bf16>(p, w, row, d, f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]}, inv, lse2);
       }
   }
   if (p.slots) attn_finish<bf16>(p, w, WAVES * kWaveRows, reinterpret_cast<float*>(smem));
@@ -228,7 +227,7 @@ template <int DP>
 hipError_t launch_dp(const PagedAttnP& p, hipStream_t st) {
   const dim3 grid((unsigned)((long)p.B * p.Hkv * p.row_tiles * p.splits));
   const auto go = [&](auto kernel) { kernel<<<grid, kPromptWaves * 64, 4 * kTile * DP * 2, st>>>(p); };
-  go(p.D == DP ? paged_attn_prompt_kernel<DP, kPromptWaves, 1, true> : paged_attn_prompt_kernel<DP, kPromptWaves, 1, false>);
+  go(p.D == DP ? paged_attn_prompt_kernel<DP, kPromptWaves, true> : paged_attn_prompt_kernel<DP, kPromptWaves, false>);
   return hipGetLastError();
 }
 

@@ -211,3 +211,54 @@ def test_streams_and_replayed_graphs():
         torch.cuda.synchronize()
         assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
     check_attention(want, None, attention(q, k, v, table, lens))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("B,T,Hq,Hkv,D,lens", [(2, 2, 4, 2, 64, [1000, 700]), (3, 1, 2, 1, 128, [1500, 3, 900]), (1, 70, 2, 2, 64, [600])])
+def test_parts_joined_by_the_last_workgroup(dtype, B, T, Hq, Hkv, D, lens):
+    # small joins take no second launch: alone, again in the same memory, replayed, and on two streams at once
+    q, k, v, table, lens = inputs(B, T, Hq, Hkv, D, 16, dtype, lens, cols=100)
+    run(q, k, v, table, lens)
+    outs, graphs, streams = [torch.zeros_like(q) for _ in range(2)], [], [torch.cuda.Stream() for _ in range(2)]
+    for out, s in zip(outs, streams):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                tsd.paged_attn_static(q, k, v, table, lens, out=out)
+                q_next = out * 2
+                tsd.paged_attn_static(q_next, k, v, table, lens, out=out)
+            graphs.append((g, q_next))
+    for step in range(20):
+        q.normal_()
+        torch.cuda.synchronize()
+        want = tsd.paged_attn_static(tsd.paged_attn_static(q, k, v, table, lens) * 2, k, v, table, lens)
+        for s, (g, _) in zip(streams, graphs):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+    check_attention(want, None, attention(tsd.paged_attn_static(q, k, v, table, lens) * 2, k, v, table, lens))
+
+
+@pytest.mark.parametrize("rows", [33, 40, 64, 65, 128, 129])
+def test_row_tiles(rows):
+    # wide heads and workgroups enough: tiles of 128 rows, some of whose wavefronts have none
+    B, Hkv = 70, 1
+    run(*inputs(B, rows, Hkv, Hkv, 128, 16, BF, [130 + (11 * i) % 90 for i in range(B)]))
+
+
+def test_maxima_that_rise_slowly_and_at_once():
+    # a row's later keys outweigh its earlier ones by a little at a time, or by far: the running maximum may lag behind, the result may not
+    B, T, D, n = 2, 130, 128, 700
+    q, k, v, table, lens = inputs(B, T, 1, 1, D, 16, BF, [n, n])
+    q[:] = 0
+    q[..., 0] = 8.0
+    for b in range(B):
+        for j in range(n):
+            at = int(table[b, j // 16]), j % 16
+            k[at] = 0
+            k[at][0, 0] = j * 0.02 if b == 0 else (0.0 if j < 400 else 60.0)
+    for scale in (None, 1.0, -1.0):
+        run(q, k, v, table, lens, scale=scale)

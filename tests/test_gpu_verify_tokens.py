@@ -146,3 +146,28 @@ def test_replayed_graph_and_streams():
         n, tokens = verified(draft, q, p, u)
         assert got["n_acc"].tolist() == n and got["tokens"].tolist() == tokens
         check(draft, q, p, u)
+
+
+@pytest.mark.parametrize("dtype", [FP, BF])
+@pytest.mark.parametrize("B,V", [(1, 40000), (3, 131072), (130, 33000)])
+def test_rows_shared_by_workgroups(dtype, B, V):
+    # the last workgroup of a row draws: again in the same memory, replayed, and with nothing left of p over q
+    draft, q, p, u = inputs(B, 2, V, dtype)
+    check(draft, q, p, u)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            got = [tsd.verify_tokens_static(draft, q, p, u), tsd.verify_tokens_static(draft, None, p, u)]
+    torch.cuda.synchronize()
+    for step in range(5):
+        u.uniform_()
+        if step == 3:
+            p[0], q[0] = 2.0 ** -18, 2.0 ** -17
+        g.replay()
+        torch.cuda.synchronize()
+        for x, by in zip(got, (q, None)):
+            n, tokens = verified(draft, by, p, u)
+            assert x["n_acc"].tolist() == n and x["tokens"].tolist() == tokens
+        check(draft, q, p, u)
