@@ -363,6 +363,7 @@ size_t attn_bytes(const AttnPlan& a, int B, int T, int Hq, int Hkv, int D) {
 }  // namespace
 
 hipError_t launch_paged_attn_bf16(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
+  if (p.D <= 32) return launch_dp<32>(p, mt, waves, st);
   if (p.D <= 64) return launch_dp<64>(p, mt, waves, st);
   if (p.D <= 96) return launch_dp<96>(p, mt, waves, st);
   if (p.D <= 128) return launch_dp<128>(p, mt, waves, st);
@@ -394,7 +395,9 @@ extern "C" int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, in
   const size_t need = attn_bytes(a, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim);
   if (need && (!workspace_dev || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
     return fail_no_handle(TSD_E_INVALID_ARG, "workspace: needs the bytes that tsd_paged_attn_workspace gives for these sizes, 16-byte aligned");
-  if ((int64_t)B * cache->n_kv_heads * a.row_tiles * a.splits > INT32_MAX) return fail_no_handle(TSD_E_OUT_OF_RANGE, "more than 2^31 workgroups");
+  if ((int64_t)B * cache->n_kv_heads * a.row_tiles * a.splits > max_workgroups(64 * kAttnWaves) ||
+      (a.splits > 1 && (int64_t)B * T * n_q_heads > max_workgroups(256)))
+    return fail_no_handle(TSD_E_OUT_OF_RANGE, "more than 2^24 - 1 workgroups");
   PagedAttnP p;
   p.cache = cache_view(*cache);
   p.q = rows_view(*q);

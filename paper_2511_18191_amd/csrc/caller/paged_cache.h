@@ -40,6 +40,9 @@ __device__ __forceinline__ long paged_row(const PagedView& c, int entry, int slo
 }
 #endif
 
+// A launch has fewer than 2^32 lanes.
+constexpr int64_t max_workgroups(int lanes) { return 0xFFFFFFFFll / lanes; }
+
 inline int type_bytes(int dtype) { return dtype == TSD_BF16 ? 2 : 4; }
 
 // 16-byte loads: rows start on 16 bytes, whatever the strides.

@@ -153,7 +153,7 @@ extern "C" int tsd_rope_append_static(const tsd_paged_cache* cache, int32_t B, i
   int rc = check_cache(cache);
   if (rc) return rc;
   const int es = type_bytes(cache->dtype);
-  if ((int64_t)B * T > INT32_MAX) return fail_no_handle(TSD_E_OUT_OF_RANGE, "B * T beyond 2^31 - 1");
+  if ((int64_t)B * T > max_workgroups(256)) return fail_no_handle(TSD_E_OUT_OF_RANGE, "B * T beyond 2^24 - 1 tokens");
   if (n_q_heads < 1 || n_q_heads > 1024) return fail_no_handle(TSD_E_INVALID_ARG, "n_q_heads must be 1..1024");
   if ((rc = check_rows(q, es, "q")) || (rc = check_rows(q_out, es, "q_out")) || (rc = check_rows(k, es, "k")) || (rc = check_rows(v, es, "v"))) return rc;
   if (!base_dev || !freq_dev) return fail_no_handle(TSD_E_INVALID_ARG, "base_dev and freq_dev must not be NULL");

@@ -293,7 +293,7 @@ int check_verify(int dtype, int32_t B, int32_t K, int32_t V) {
   if (dtype != TSD_F32 && dtype != TSD_BF16) return fail_no_handle(TSD_E_INVALID_ARG, "dtype must be TSD_F32 or TSD_BF16");
   if (B < 1 || K < 1 || V < 1) return fail_no_handle(TSD_E_INVALID_ARG, "need B >= 1, K >= 1, V >= 1");
   if (K > kMaxDrafts) return fail_no_handle(TSD_E_OUT_OF_RANGE, "at most 16 drafts");
-  if ((int64_t)B * ((V + (int64_t)kSegment - 1) / kSegment + 3) > INT32_MAX) return fail_no_handle(TSD_E_OUT_OF_RANGE, "B * V beyond what a launch takes");
+  if (B > max_workgroups(1024) || (int64_t)B * (V / kSegment + 4) > INT32_MAX) return fail_no_handle(TSD_E_OUT_OF_RANGE, "B, or B * V, beyond what a launch takes");
   return TSD_OK;
 }
 

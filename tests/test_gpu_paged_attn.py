@@ -262,3 +262,11 @@ def test_maxima_that_rise_slowly_and_at_once():
             k[at][0, 0] = j * 0.02 if b == 0 else (0.0 if j < 400 else 60.0)
     for scale in (None, 1.0, -1.0):
         run(q, k, v, table, lens, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [8, 24, 32, 72, 96, 120, 128, 136, 192, 256])
+def test_head_sizes(dtype, D):
+    # few rows and many, one key head for three query heads
+    for T, lens in ((2, [50, 300]), (45, [45, 200])):
+        run(*inputs(2, T, 3, 1, D, 16, dtype, lens))
