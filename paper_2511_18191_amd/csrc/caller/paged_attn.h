@@ -1,6 +1,7 @@
-// Attention of new tokens over a caller's paged cache: what its kernels share (paged_attn.hip on bf16 caches, paged_attn_f32.hip on fp32 ones).
+// Attention of new tokens over a caller's paged cache: what its kernels share (paged_attn.hip on bf16 caches,
+// paged_attn_prompt.hip on bf16 caches where rows are many, paged_attn_f32.hip on fp32 ones).
 //
-// Rows: the T new tokens and the G = Hq / Hkv query heads of one key head are rows t * G + g of one product, in tiles of 16 * MT, so that a
+// Rows: the T new tokens and the G = Hq / Hkv query heads of one key head are rows t * G + g of one product, in tiles, so that a
 // key head's keys and values are read once for all of them.  Row of token t sees keys j < len - n_new + t + 1.
 //
 // Split: the keys of a sequence go in chunks of `chunk`; a workgroup takes one (sequence, key head, row tile, chunk), its wavefronts take
