@@ -251,7 +251,7 @@ int tsd_accept_commit_static(const float* X_dev, const float* mu_q_dev, const fl
  * back is holding fewer tokens: base + n_acc + 1, and what the cache has behind them is overwritten by the next round.
  * They need no handle, allocate nothing, free nothing and keep nothing; everything is asynchronous on `stream`, whose device must be the
  * current one, and may be captured into a graph.  Host checks come first; what only the device knows (lengths, pages, tokens) is
- * bounded there, as said at each call, and never read or written out of range. */
+ * bounded there, as said at each call, and never read or written out of range.  For serving: nothing here has a gradient. */
 
 /* A caller's paged cache.  Token j of sequence b has its keys and values at page page_table_dev[b * table_stride + j / page_tokens], row
  * j % page_tokens: element offset page * page_stride + row * token_stride + head * head_stride in both pools, head_dim elements in a row.
@@ -302,6 +302,7 @@ int tsd_rope_append_static(const tsd_paged_cache* cache, int32_t B, int32_t T, i
 
 /* Causal attention of the last n_new tokens of each sequence over the cache that holds them: token t of sequence b sees the keys
  * j < lens_dev[b] - n_new + t + 1, out = sum_j softmax_j(scale q . k_j) v_j, query head h with key head h / (n_q_heads / n_kv_heads).
+ * out may be q (the same data and strides) and must not overlap it otherwise.
  * n_new_dev int32 [B] (NULL: T each; clamped to 0..T); rows behind them are left as they were.  A row that sees no key (an empty
  * sequence, holes only, scores of -inf only) gives zeros.  What the cache holds where a row does not look, not finite or never written, does not reach it.
  * lse_dev (nullable): float [B][T][n_q_heads], the logarithm of the softmax's denominator (-inf for empty rows).

@@ -222,7 +222,8 @@ def paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len=None, scale=N
     """tsd_paged_attn_static on torch's current stream of the tensors' device: the last n_new (None: T each) tokens of every sequence attend
     to the lens[b] tokens its pages hold, themselves among them.  Tensors as for rope_append_static; lens int32 [B]; max_len: the longest of lens
     as far as the host knows (None: what the table has room for); scale: None for 1 / sqrt(head_dim).  Returns out, or (out, lse [B, T,
-    heads]) with want_lse; rows behind n_new are left as they were, in a new tensor they hold nothing.  The workspace is allocated here."""
+    heads]) with want_lse; out may be q; rows behind n_new are left as they were, in a new tensor they hold nothing.  The workspace is
+    allocated here."""
     if _calls is None:
         _bind_calls()
     if max_len is not None and max_len < 1:

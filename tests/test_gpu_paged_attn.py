@@ -270,3 +270,14 @@ def test_head_sizes(dtype, D):
     # few rows and many, one key head for three query heads
     for T, lens in ((2, [50, 300]), (45, [45, 200])):
         run(*inputs(2, T, 3, 1, D, 16, dtype, lens))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("B,T,D,lens", [(2, 3, 64, [70, 20]), (2, 2, 64, [900, 700]), (1, 5, 128, [9000]), (1, 200, 128, [700])])
+def test_out_may_be_q(dtype, B, T, D, lens):
+    # whole, joined by the last workgroup, joined by a second launch, many rows
+    q, k, v, table, lens = inputs(B, T, 4, 2, D, 16, dtype, lens)
+    want = tsd.paged_attn_static(q, k, v, table, lens)
+    got = q.clone()
+    assert tsd.paged_attn_static(got, k, v, table, lens, out=got) is not None
+    assert torch.equal(got, want)
