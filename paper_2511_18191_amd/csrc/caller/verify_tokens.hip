@@ -9,7 +9,7 @@
 // row's segments are dealt to several (some 512 in all), and the one that comes last goes on (last_arriver.h).  Rows start anywhere (an
 // odd vocabulary), so 16-byte loads need no alignment beyond the element's.
 // Three dependent trips to memory (drafts, their probabilities, the rows), 3 us, bound small calls: 1 x 4 drafts, 32000 fp32 probabilities
-// 7.7 us; 64 x 6, 131072 fp32 16.9 us (58 MB: 3.4 TB/s); 256 x 8, 50257 bf16 14.4 us (41 MB: 2.8 TB/s).
+// 7.3 us; 64 x 6, 131072 fp32 16.4 us (58 MB: 3.5 TB/s); 256 x 8, 50257 bf16 14.0 us (41 MB: 2.9 TB/s).
 #include <algorithm>
 
 #include "last_arriver.h"
@@ -242,7 +242,7 @@ __device__ __forceinline__ long find_token(const Weights<T>& w, const Found& f, 
   return __shfl(heavy, 63 - __builtin_clzll(who));
 }
 
-// ONE: a workgroup sums a whole row, into LDS.  Else the row's workgroups sum a segment per wavefront, and the last of them draws.
+// ONE: a workgroup sums a whole row, into LDS.  Else a row's workgroups sum `per` segments each, and the last of them draws.
 template <typename T, int WAVES, bool ONE>
 __global__ __launch_bounds__(WAVES * 64) void verify_kernel(const VerifyP a) {
   __shared__ double own_sums[ONE ? kOneSegments : 1];
