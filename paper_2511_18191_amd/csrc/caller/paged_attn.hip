@@ -321,11 +321,11 @@ struct AttnPlan {
 
 AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len) {
   AttnPlan a;
-  const int rows = T * (Hq / Hkv);
+  const int64_t rows = (int64_t)T * (Hq / Hkv);
   a.prompt = dtype == TSD_BF16 && D <= 128 && (rows > 64 || (rows > 32 && D > 96 && (int64_t)B * Hkv >= 64));
   a.mt = rows <= 16 || D > 128 ? 1 : 2;
   const int tile_rows = a.prompt ? kPromptRows : 16 * a.mt;
-  a.row_tiles = (rows + tile_rows - 1) / tile_rows;
+  a.row_tiles = (int)((rows + tile_rows - 1) / tile_rows);
   const int64_t base = (int64_t)B * Hkv * a.row_tiles, steps = (max_len + 31) / 32;  // workgroups where nothing is split
   a.waves = a.prompt ? kPromptWaves : (int)std::min<int64_t>(base >= 1024 && steps <= 4 ? 1 : D > 128 ? 2 : kAttnWaves, steps);
   const int64_t step = a.prompt ? 64 : 32 * a.waves;
@@ -336,11 +336,11 @@ AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len)
     chunk = chunk < step + step / 4 ? step : (chunk + step - 1) / step * step;
   }
   if (a.prompt) chunk = std::max<int64_t>(chunk, 256);
-  chunk = std::max(chunk, max_len * base / 16384);
-  chunk = std::max(step, (chunk + step - 1) / step * step);
+  chunk = std::min<int64_t>(std::max(chunk, max_len * base / 16384), max_len);  // (a sequence that stays whole: no longer than it is)
+  chunk = (chunk + step - 1) / step * step;
   a.chunk = (int)chunk;
-  a.splits = (max_len + a.chunk - 1) / a.chunk;
-  a.joins = a.splits > 1 && a.splits <= 16 && base < 256 && a.splits * std::min(rows, tile_rows) * D <= 16384;
+  a.splits = (int)((max_len + chunk - 1) / chunk);
+  a.joins = a.splits > 1 && a.splits <= 16 && base < 256 && a.splits * std::min<int64_t>(rows, tile_rows) * D <= 16384;
   return a;
 }
 
