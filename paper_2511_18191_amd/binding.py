@@ -107,7 +107,7 @@ SYMBOLS = {
     "tsd_set_sigma": ([C.c_void_p, C.c_float, C.c_float], C.c_int),
 }
 
-_lib = _calls = None
+_lib = _calls = _round_calls = None
 
 
 def library_path():
@@ -136,7 +136,7 @@ def lib():
 
 def _bind_calls():
     """Load the extension beside the library (building it first only if it does not exist) and hand it the library's entries."""
-    global _calls
+    global _calls, _round_calls
     handle = lib()
     from . import build as _build
     if not os.path.exists(_build.CALLS):
@@ -144,10 +144,19 @@ def _bind_calls():
         importlib.invalidate_caches()
     from . import _torch_calls
     _torch_calls.bind(C.cast(handle.tsd_accept_commit_static, C.c_void_p).value)
-    _torch_calls.bind_round(*(C.cast(getattr(handle, name), C.c_void_p).value for name in (
-        "tsd_rope_append_static", "tsd_paged_attn_workspace", "tsd_paged_attn_static", "tsd_verify_tokens_workspace",
-        "tsd_verify_tokens_static")))
+    if hasattr(_torch_calls, "bind_round"):  # (a file of an older build has the acceptance call only)
+        _torch_calls.bind_round(*(C.cast(getattr(handle, name), C.c_void_p).value for name in (
+            "tsd_rope_append_static", "tsd_paged_attn_workspace", "tsd_paged_attn_static", "tsd_verify_tokens_workspace",
+            "tsd_verify_tokens_static")))
+        _round_calls = _torch_calls
     _calls = _torch_calls
+
+
+def _bind_round_calls():
+    if _calls is None:
+        _bind_calls()
+    if _round_calls is None:
+        raise RuntimeError("_torch_calls.so is older than this package: build it again (python -m paper_2511_18191_amd.build)")
 
 
 def make_config(target, draft, patch, K, max_batch, max_tokens, dtype, sigma_p, sigma_q=None, seed=0,
@@ -210,9 +219,9 @@ def rope_append_static(q, k, v, k_pool, v_pool, page_table, base, freq, position
     permuted view holds a cache in another order); page_table int32 [B, pages per sequence]; base int32 [B], the tokens held so far; freq
     from rope_frequencies; positions int32 [B, T] and n_new int32 [B] or None.  The pools are written in place; returns the rotated
     queries: `out` (q itself to rotate in place), or a new tensor, whose rows behind n_new hold nothing."""
-    if _calls is None:
-        _bind_calls()
-    rc, out = _calls.rope_append_static(q, k, v, k_pool, v_pool, page_table, base, freq, positions, n_new, interleaved, amplitude, out)
+    if _round_calls is None:
+        _bind_round_calls()
+    rc, out = _round_calls.rope_append_static(q, k, v, k_pool, v_pool, page_table, base, freq, positions, n_new, interleaved, amplitude, out)
     if rc:
         _check(rc)
     return out
@@ -224,13 +233,13 @@ def paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len=None, scale=N
     as far as the host knows (None: what the table has room for); scale: None for 1 / sqrt(head_dim).  Returns out, or (out, lse [B, T,
     heads]) with want_lse; out may be q; rows behind n_new are left as they were, in a new tensor they hold nothing.  The workspace is
     allocated here."""
-    if _calls is None:
-        _bind_calls()
+    if _round_calls is None:
+        _bind_round_calls()
     if max_len is not None and max_len < 1:
         raise ValueError("max_len must be at least 1")
     if scale is not None and scale != scale:
         raise ValueError("scale must be finite")
-    rc, out, lse = _calls.paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len or 0, float("nan") if scale is None else scale, n_new,
+    rc, out, lse = _round_calls.paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len or 0, float("nan") if scale is None else scale, n_new,
                                             out, want_lse)
     if rc:
         _check(rc)
@@ -241,9 +250,9 @@ def verify_tokens_static(draft, q, p, uniforms, n_draft=None):
     """tsd_verify_tokens_static on torch's current stream of the tensors' device.  draft: int32 or int64 [B, K]; q: [B, K, V] or None (certain
     drafts), p: [B, K + 1, V], float32 or bfloat16, rows dense; uniforms: float32 [B, K + 1] in [0, 1), the last of a row for the draw;
     n_draft: int32 [B] or None.  Returns dict(n_acc int32 [B], tokens [B, K + 1]): the drafts that passed, the drawn token, -1 behind it."""
-    if _calls is None:
-        _bind_calls()
-    rc, n_acc, tokens = _calls.verify_tokens_static(draft, q, p, uniforms, n_draft)
+    if _round_calls is None:
+        _bind_round_calls()
+    rc, n_acc, tokens = _round_calls.verify_tokens_static(draft, q, p, uniforms, n_draft)
     if rc:
         _check(rc)
     return dict(n_acc=n_acc, tokens=tokens)
