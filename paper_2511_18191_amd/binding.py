@@ -218,7 +218,8 @@ def rope_append_static(q, k, v, k_pool, v_pool, page_table, base, freq, position
     pools: [pages, page_tokens, kv_heads, head_dim], all float32 or bfloat16 with a dense last dimension and any 16-byte strides (a
     permuted view holds a cache in another order); page_table int32 [B, pages per sequence]; base int32 [B], the tokens held so far; freq
     from rope_frequencies; positions int32 [B, T] and n_new int32 [B] or None.  The pools are written in place; returns the rotated
-    queries: `out` (q itself to rotate in place), or a new tensor, whose rows behind n_new hold nothing."""
+    queries: `out` (q itself to rotate in place), or a new tensor, whose rows behind n_new hold nothing.  No gradients: while they are
+    recorded, tensors that want one are refused."""
     if _round_calls is None:
         _bind_round_calls()
     rc, out = _round_calls.rope_append_static(q, k, v, k_pool, v_pool, page_table, base, freq, positions, n_new, interleaved, amplitude, out)
@@ -232,7 +233,7 @@ def paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len=None, scale=N
     to the lens[b] tokens its pages hold, themselves among them.  Tensors as for rope_append_static; lens int32 [B]; max_len: the longest of lens
     as far as the host knows (None: what the table has room for); scale: None for 1 / sqrt(head_dim).  Returns out, or (out, lse [B, T,
     heads]) with want_lse; out may be q; rows behind n_new are left as they were, in a new tensor they hold nothing.  The workspace is
-    allocated here."""
+    allocated here.  No gradients, as for rope_append_static."""
     if _round_calls is None:
         _bind_round_calls()
     if max_len is not None and max_len < 1:

@@ -8,6 +8,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -180,6 +181,15 @@ int dtype_of(const at::Tensor& t, const char* name) {
   return t.scalar_type() == at::kFloat ? TSD_F32 : TSD_BF16;
 }
 
+// Nothing here has a gradient, and none is to be lost unsaid.
+void no_gradient(const at::Tensor& t, const char* name) {
+  NEED(!t.requires_grad(), std::string(name) + " wants a gradient, which this call does not have: call it under torch.no_grad(), or with detached tensors");
+}
+// A tensor that a call wrote counts as changed in place (those of inference mode have no count).
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // [B, T, heads, head_dim] with dense heads (dimensions of one step have no stride that matters)
 tsd_rows rows_of(const at::Tensor& t, at::IntArrayRef sizes, const char* name) {
   NEED(t.sizes() == sizes, std::string(name) + " has another shape than its call's");
@@ -248,6 +258,15 @@ PyObject* rope_append_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int inter = PyObject_IsTrue(args[10]);
     const double amplitude = PyFloat_AsDouble(args[11]);
     if (PyErr_Occurred()) return nullptr;
+    if (c10::GradMode::is_enabled()) {
+      no_gradient(q, "q");
+      no_gradient(k, "k");
+      no_gradient(v, "v");
+      no_gradient(k_pool, "k_pool");
+      no_gradient(v_pool, "v_pool");
+      no_gradient(freq, "freq");
+      if (to) no_gradient(*to, "out");
+    }
     NEED(q.dim() == 4, "q must be [B, T, heads, head_dim]");
     const int64_t B = q.size(0), T = q.size(1);
     tsd_paged_cache cache = cache_of(k_pool, v_pool, table, B);
@@ -277,6 +296,11 @@ PyObject* rope_append_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
                    n_new ? static_cast<const int32_t*>(n_new->data_ptr()) : nullptr, positions ? static_cast<const int32_t*>(positions->data_ptr()) : nullptr,
                    static_cast<const double*>(freq.data_ptr()), r, (float)amplitude, inter ? TSD_FLAG_ROPE_INTERLEAVED : 0, stream);
     Py_END_ALLOW_THREADS
+    if (rc == TSD_OK) {
+      written(k_pool);
+      written(v_pool);
+      if (to) written(out);
+    }
     return Py_BuildValue("iN", rc, THPVariable_Wrap(out));
   });
 }
@@ -292,6 +316,12 @@ PyObject* paged_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor *n_new = maybe(args[7], "n_new"), *to = maybe(args[8], "out");
     const int want_lse = PyObject_IsTrue(args[9]);
     if (PyErr_Occurred()) return nullptr;
+    if (c10::GradMode::is_enabled()) {
+      no_gradient(q, "q");
+      no_gradient(k_pool, "k_pool");
+      no_gradient(v_pool, "v_pool");
+      if (to) no_gradient(*to, "out");
+    }
     NEED(q.dim() == 4, "q must be [B, T, heads, head_dim]");
     const int64_t B = q.size(0), T = q.size(1), H = q.size(2);
     tsd_paged_cache cache = cache_of(k_pool, v_pool, table, B);
@@ -319,6 +349,7 @@ PyObject* paged_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
       rc = attn_fn(&cache, b, t, h, &rq, &ro, want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, static_cast<const int32_t*>(lens.data_ptr()),
                    n_new ? static_cast<const int32_t*>(n_new->data_ptr()) : nullptr, max_len, (float)scale, bytes ? work.data_ptr() : nullptr, bytes, stream);
       Py_END_ALLOW_THREADS
+      if (rc == TSD_OK && to) written(out);
     }
     PyObject* l = want_lse ? THPVariable_Wrap(lse) : Py_None;
     if (!want_lse) Py_INCREF(Py_None);
