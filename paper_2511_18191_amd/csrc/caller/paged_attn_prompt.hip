@@ -6,7 +6,12 @@
 //   O^T += V^T P^T the contraction's order is free, so those same keys are its operand as they lie, and V rows are picked up transposed for
 //                  them (ds_read_b64_tr_b16: 4 keys of one dim).
 // Maximum, sum and rescaling of a row stay in its two lanes: one exchange between the halves per 64 keys, and nothing crosses lanes for the
-// sums.  The weights are rounded to bf16, the instruction's operand; their sum is not.
+// sums.  The weights are rounded to bf16, the instruction's operand, and the sum is that of the rounded ones, as in paged_attn.hip, by the dot product
+// of two weights with ones (rounded once, to fp32).  The heaviest weight is 1 and exact: sums are rescaled by every key that is the largest
+// so far.  Where the logarithm of the denominator is asked for, the unrounded weights are summed beside, and it (and the join of parts) is of these.
+// (Sums relative to a maximum that lagged by up to 2^6, of unrounded weights, took 77 us for 81 with 2 x 1024 tokens over 2048 keys, 32 heads over 8 of
+// 128, and 41 for 44 with 16 heads of 64, and were less exact: scores of deviation 1.5, 4, 8 were off by 2.21, 1.86, 1.73 in 1000 where this is by
+// 1.92, 1.68, 1.64, and the result's rounding alone by 1.66, 1.67, 1.64.)
 // 32 rows a wavefront at 252 registers, two on a SIMD: one forms weights while the other multiplies.  (64 rows would read LDS half as often, but
 // do not fit: 350 registers and spills.)
 // 2 x 1024 tokens behind 2048, 32 heads over 8 of 128: 110 us, 0.78 PFLOP/s; weights and products overlap only in part, and both take some
@@ -16,8 +21,7 @@
 namespace tsd {
 namespace {
 
-constexpr int kTile = 64;      // keys a tile
-constexpr float kLag = 6.f;    // weights up to 64: bf16's steps and fp32's sums are as fine there
+constexpr int kTile = 64;  // keys a tile
 
 // 16-byte chunk `c` of row `r` lies at chunk c ^ turn(r) of its row: one chunk of 16 rows, and four of 4, cover all 256 bytes of the banks.
 template <int DP>
@@ -25,7 +29,7 @@ __device__ __forceinline__ int turn(int r) {
   return DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
 }
 
-template <int DP, int WAVES, bool FULL>  // FULL: head_dim is DP
+template <int DP, int WAVES, bool FULL, bool LSE>  // FULL: head_dim is DP; LSE: the logarithms are asked for
 __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int kWaveRows = 32, KK = DP / 16, DB = DP / 32, CPR = DP / 8, THREADS = WAVES * 64, NL = kTile * CPR / THREADS;
@@ -59,7 +63,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
   const int see_last = row0 < w.rows ? attn_sees(p, w, min(row0 + kWaveRows, w.rows) - 1) : 0;
 
   f32x16 o[DB];
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = -INFINITY, l_run = 0.f, l_true = 0.f;  // (l_true: of the unrounded weights)
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -148,8 +152,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
 #pragma unroll
     for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
     mx = fmaxf(mx, __shfl_xor(mx, 32));
-    // Sums are kept relative to a maximum that may lag by a factor of 2^kLag: most tiles raise some row's by a little, and leave the sums alone.
-    const bool raise = (mx - m_run) * scale2 > kLag;  // (the first key a row sees, too)
+    const bool raise = mx > m_run;  // (the first key a row sees, too)
     if (__any(raise)) {
       float alpha = 1.f;
       if (raise) {
@@ -157,6 +160,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
         m_run = mx;
       }
       l_run *= alpha;
+      if (LSE) l_true *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -170,9 +174,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float e = __builtin_amdgcn_exp2f(fmaf(sc[s][i], scale2, shift));
-        l_run += e;
+        if (LSE) l_true += e;
         pf[i >> 3][i & 7] = (bf16)e;
       }
+      typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      const bf16x2 ones = {(bf16)1.f, (bf16)1.f};
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[i >> 3][i & 7], pf[i >> 3][(i & 7) + 1]}, ones, l_run, false);
       // operand of the values: keys 16 m + 8 (j / 4) + 4 h + j % 4, j = 0 .. 7, for dim lane % 32 of a block
 #pragma unroll
       for (int m = 0; m < 2; ++m)
@@ -208,10 +216,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
     }
   }
 
-  const float sum = l_run + __shfl_xor(l_run, 32);
+  const float sum = l_run + __shfl_xor(l_run, 32), true_sum = LSE ? l_true + __shfl_xor(l_true, 32) : sum;
   if (row < w.rows) {
     const bool none = sum == 0.f;
-    const float inv = none ? 0.f : 1.f / sum, lse2 = none ? -INFINITY : m_run * scale2 + __builtin_amdgcn_logf(sum);
+    const float inv = none ? 0.f : 1.f / sum, lse2 = none ? -INFINITY : m_run * scale2 + __builtin_amdgcn_logf(true_sum);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -227,7 +235,10 @@ template <int DP>
 hipError_t launch_dp(const PagedAttnP& p, hipStream_t st) {
   const dim3 grid((unsigned)((long)p.B * p.Hkv * p.row_tiles * p.splits));
   const auto go = [&](auto kernel) { kernel<<<grid, kPromptWaves * 64, 4 * kTile * DP * 2, st>>>(p); };
-  go(p.D == DP ? paged_attn_prompt_kernel<DP, kPromptWaves, true> : paged_attn_prompt_kernel<DP, kPromptWaves, false>);
+  if (p.lse)
+    go(p.D == DP ? paged_attn_prompt_kernel<DP, kPromptWaves, true, true> : paged_attn_prompt_kernel<DP, kPromptWaves, false, true>);
+  else
+    go(p.D == DP ? paged_attn_prompt_kernel<DP, kPromptWaves, true, false> : paged_attn_prompt_kernel<DP, kPromptWaves, false, false>);
   return hipGetLastError();
 }
 
