@@ -7,7 +7,7 @@
 // Split: the keys of a sequence go in chunks of `chunk`; a workgroup takes one (sequence, key head, row tile, chunk), its wavefronts take
 // its steps of 32 keys in turn, each with a running maximum and sum of its own, joined in LDS at the end.  Where a sequence may
 // have several chunks, each leaves its rows' normalised sums and their logarithm (base 2) in the workspace.  They are joined by the workgroup
-// of a (sequence, key head, row tile) that comes last (last_arriver.h), or, where that is much for one workgroup, by a second launch.
+// of a (sequence, key head, row tile) that comes last (last_arriver.h), or, where that is much for one workgroup or rows are many, by a second launch.
 #pragma once
 #include "last_arriver.h"
 #include "paged_cache.h"

@@ -306,11 +306,15 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // 36 x 896 42.9), none shorter than a step of all wavefronts, and of at most 1024 keys where up to four workgroups a compute unit would
 // otherwise go by the longest sequence (64 ragged sequences of up to 8192: whole 239 us, 1024 keys 217, 256 keys 256).  With more
 // workgroups than that, sequences stay whole.  At most 16384 workgroups, most of them idle, where max_len says much more than lengths are.
+// For many rows, whose parts are much to write and join, chunks are no shorter than an eighth of max_len in whole tiles of 64 keys, or than 256, and
+// up to 256 keys stay whole (128 rows of 8 heads of 64: 11.1 us, in two 14.0).  us at 512 keys with chunks of 64, 128 and 256: 68 rows of 2 heads of
+// 128 12.0, 14.7, 18.2, 300 rows of 4 of 80 14.0, 16.2, 19.8, but with 64 and 256 128 rows of 32 of 128 23.6, 20.8; at 1000 keys with 128 and 256: 128
+// rows of 8 of 128 15.1, 18.1; at 2000 keys with 128 and 256: 256 rows of 8 of 128 26.2, 20.2, 68 rows of 2 14.6, 18.2.
 // Kernel: the one for many rows from 65 rows a key head on (68 of 128, us for 64 sequences of up to 8192: 296 against 622; 120 of 80, 32 of up to 2000:
 // 51 against 67), and from 33 on where heads are wide and workgroups enough (40 of 128, 64 sequences: 278 against 435, 8: 45 against 51; but
 // 36 of 64, 128 sequences of up to 2000: 74 against 62).
 // Joins: by the last workgroup where that is little work for one (12 chunks of 9 rows of 80: 17.5 us against 19.0 with a second launch, 8 of 8 rows of
-// 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3).
+// 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3), and not for many rows (2 chunks of 128 rows of 64 24.5 and 15.4).
 // Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys
 // 45.9 us, two 46.8, four 52.0).
 struct AttnPlan {
@@ -335,12 +339,12 @@ AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len)
     chunk = std::min<int64_t>(max_len * base / 256, tall ? max_len : 1024);
     chunk = chunk < step + step / 4 ? step : (chunk + step - 1) / step * step;
   }
-  if (a.prompt) chunk = std::max<int64_t>(chunk, 256);
+  if (a.prompt) chunk = std::max(chunk, max_len <= 256 ? 256 : std::min<int64_t>(256, (max_len + 511) / 512 * 64));
   chunk = std::min<int64_t>(std::max(chunk, max_len * base / 16384), max_len);  // (a sequence that stays whole: no longer than it is)
   chunk = (chunk + step - 1) / step * step;
   a.chunk = (int)chunk;
   a.splits = (int)((max_len + chunk - 1) / chunk);
-  a.joins = a.splits > 1 && a.splits <= 16 && base < 256 && a.splits * std::min<int64_t>(rows, tile_rows) * D <= 16384;
+  a.joins = !a.prompt && a.splits > 1 && a.splits <= 16 && base < 256 && a.splits * std::min<int64_t>(rows, tile_rows) * D <= 16384;
   return a;
 }
 

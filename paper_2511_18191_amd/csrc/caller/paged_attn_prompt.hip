@@ -228,7 +228,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
         if (FULL || d < p.D) attn_store<bf16>(p, w, row, d, f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]}, inv, lse2);
       }
   }
-  if (p.slots) attn_finish<bf16>(p, w, WAVES * kWaveRows, reinterpret_cast<float*>(smem));
 }
 
 template <int DP>

@@ -53,7 +53,7 @@ def check(dtype, B, T, Hq, Hkv, D, n, heavy, seed=0, page=16):
 SIZES = [
     (1, 1, 16, 1, 64, 61), (2, 2, 4, 2, 64, 1000),                      # whole, joined in the launch
     (1, 5, 32, 8, 128, 4099), (3, 1, 8, 1, 64, 2500), (2, 3, 2, 2, 256, 1300), (1, 9, 4, 1, 80, 2000),      # a second launch; wide and odd heads
-    (1, 70, 2, 2, 64, 500), (2, 130, 1, 1, 128, 500),                   # many rows: joined in the launch, whole
+    (1, 70, 2, 2, 64, 500), (2, 130, 1, 1, 128, 500), (2, 130, 1, 1, 128, 250),      # many rows: short chunks, whole
     (1, 80, 2, 2, 128, 3100), (2, 65, 4, 1, 96, 1700), (1, 200, 2, 1, 64, 4099),
 ]
 
