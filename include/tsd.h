@@ -307,10 +307,13 @@ int tsd_rope_append_static(const tsd_paged_cache* cache, int32_t B, int32_t T, i
  * sequence, holes only, scores of -inf only) gives zeros.  What the cache holds where a row does not look, not finite or never written, does not reach it.
  * lse_dev (nullable): float [B][T][n_q_heads], the logarithm of the softmax's denominator (-inf for empty rows).
  * max_len sizes the launch: the longest of lens_dev as far as the host knows (pages_per_seq * page_tokens does); longer sequences are
- * right and slow.  Long caches with few rows are split over their length, and joined by a second launch: the sums of the parts go to
- * workspace_dev (16-byte aligned, tsd_paged_attn_workspace bytes, often 0; need not be cleared; calls that may overlap need one each).
- * bf16: products accumulate in fp32, softmax in fp32, its weights are rounded to bf16 for the product with the values.  Results depend
- * on the sizes given, not on what runs beside: repeated calls give the same bits. */
+ * right and slow.  Long caches with few rows are split over their length, and joined by the workgroup that comes last or by a second
+ * launch: the parts' sums, and the words by which that workgroup knows, are in workspace_dev (16-byte aligned, tsd_paged_attn_workspace
+ * bytes, often 0; need not be cleared; calls that may overlap need one each).
+ * bf16: products accumulate in fp32, softmax in fp32, its weights are rounded to bf16 (by up to 2^-8) for the product with the values, and out
+ * is divided by the sum of the rounded ones, so that a weight's error counts by its value's distance from out only, and the heaviest
+ * weight has none.  lse_dev may be off by the same roundings, 2^-8 at most and most often 10^-4.  Results depend on the sizes
+ * given and on whether lse_dev is, not on what runs beside: repeated calls give the same bits. */
 int tsd_paged_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, size_t* bytes_host);
 int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
                           float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, int32_t max_len, float scale,

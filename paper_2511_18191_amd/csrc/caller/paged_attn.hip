@@ -4,11 +4,12 @@
 //   S^T = K Q^T   two 16x16x32 MFMAs per 32 dims and row tile; key rows are permuted so that lane group g = lane / 16 ends up with the
 //                 scores of the 8 consecutive keys 8g .. 8g + 7 for row lane % 16, which is the A operand of the next product;
 //   online softmax in fp32, base 2 (running maximum and sum per row, shared by its 4 lanes).  The weights are rounded to bf16, the matrix
-//                 instruction's operand, and the sum is that of the rounded ones: a weight's error of 2^-9 then moves the result only by
+//                 instruction's operand, and the sum is that of the rounded ones: a weight's error of up to 2^-8 then moves the result only by
 //                 the share of its value's distance from the mean;
 //   O += P V      V rows are fetched with 16-byte loads, parked in LDS and picked up transposed with ds_read_b64_tr_b16.
 // Few rows are memory bound: the next step's keys and values are asked for before this one's softmax, into the registers that its own
-// left.  One token of 64 sequences of 100 to 8192 keys, 32 heads over 8 of 128: 217 us, 5.0 TB/s (a copy reaches 5.1); 7 tokens of 512 sequences
+// left.  One token of 64 sequences of 100 to 8192 keys, 32 heads over 8 of 128: 212 us for 254387 keys in all, 4.9 TB/s (a copy reaches 5.2, eight other
+// draws of lengths 195 to 237 us, 4.7 to 5.0); 16 heads over 4 of 256, 2000 keys each: 97 us, 5.4 TB/s; 7 tokens of 512 sequences
 // of 80 keys, 16 heads of 64: 44 us, 4.1 TB/s, a wavefront's three steps behind two trips for its lengths and pages; 5 tokens of one
 // sequence of 32768 keys, 32 heads over 8 of 128: 36.5 us, 3.7 TB/s, of which the join is 5 and the first and last trips some 6.
 #include <algorithm>
@@ -310,9 +311,10 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // up to 256 keys stay whole (128 rows of 8 heads of 64: 11.1 us, in two 14.0).  us at 512 keys with chunks of 64, 128 and 256: 68 rows of 2 heads of
 // 128 12.0, 14.7, 18.2, 300 rows of 4 of 80 14.0, 16.2, 19.8, but with 64 and 256 128 rows of 32 of 128 23.6, 20.8; at 1000 keys with 128 and 256: 128
 // rows of 8 of 128 15.1, 18.1; at 2000 keys with 128 and 256: 256 rows of 8 of 128 26.2, 20.2, 68 rows of 2 14.6, 18.2.
-// Kernel: the one for many rows from 65 rows a key head on (68 of 128, us for 64 sequences of up to 8192: 296 against 622; 120 of 80, 32 of up to 2000:
-// 51 against 67), and from 33 on where heads are wide and workgroups enough (40 of 128, 64 sequences: 278 against 435, 8: 45 against 51; but
-// 36 of 64, 128 sequences of up to 2000: 74 against 62).
+// Kernel: the one for many rows from 65 rows a key head on (68 of 8 heads of 128, us for 64 sequences of up to 8192: 296 against 629; 120 of 4 of 80, 32
+// of up to 2000: 54 against 68), and from 33 on where heads are wide and workgroups enough (40 of 8 of 128, 64 sequences: 276 against 441, 8: 49
+// against 66; but 36 of 4 of 64, 128 sequences of up to 2000: 62 and 62).  Heads above 128 have none: 2 x 1024 tokens behind 2048, 16 heads over 4 of
+// 256, take 423 us (0.20 PFLOP/s) in tiles of 16 rows.
 // Joins: by the last workgroup where that is little work for one (12 chunks of 9 rows of 80: 17.5 us against 19.0 with a second launch, 8 of 8 rows of
 // 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3), and not for many rows (2 chunks of 128 rows of 64 24.5 and 15.4).
 // Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys

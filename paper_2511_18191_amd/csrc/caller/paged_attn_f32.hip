@@ -3,8 +3,10 @@
 //   S^T = K Q^T   lane group g takes 4 consecutive dims in one load, one per instruction (which dims an instruction contracts is free);
 //                 lane (q, g) ends up with keys 4g .. 4g + 3 of each 16 for row q: the A operand of the next product, a key per instruction;
 //   O += P V      lane (i, g) holds dims 4i .. 4i + 3 of every 64 of its key's row, one per instruction: no transposition.
-// One token of 64 sequences of 2000 keys, 32 heads over 8 of 128: 184 us, 5.7 TB/s.  2 x 1024 tokens behind 2048, same heads: 935 us, 92 of the
-// instruction's 148 TFLOP/s.  Short calls are bound by latency: 32 keys of 128 dims are two chains of 32 dependent instructions, 1 us.
+// One token of 64 sequences of 2000 keys, 32 heads over 8 of 128: 185 us, 5.7 TB/s; 16 over 4 of 256: 188 us, 5.6.  2 x 1024 tokens behind 2048, 32 heads
+// over 8 of 128: 934 us, 92 of the 148 TFLOP/s that a large product reaches: keys and values are fetched for every 32 rows; 16 over 4 of 256, where
+// registers spill (64 bytes of scratch a lane, 136 below 256 dims): 1051 us, 82.  Short calls are bound by the matrix instructions of a step, 128 of
+// 32 clocks for 80 dims as for 128, and three trips to memory.
 #include "paged_attn.h"
 
 namespace tsd {

@@ -14,8 +14,8 @@
 // 1.92, 1.68, 1.64, and the result's rounding alone by 1.66, 1.67, 1.64.)
 // 32 rows a wavefront at 252 registers, two on a SIMD: one forms weights while the other multiplies.  (64 rows would read LDS half as often, but
 // do not fit: 350 registers and spills.)
-// 2 x 1024 tokens behind 2048, 32 heads over 8 of 128: 110 us, 0.78 PFLOP/s; weights and products overlap only in part, and both take some
-// 1000 clocks per 64 keys and 32 rows.
+// 2 x 1024 tokens behind 2048, 32 heads over 8 of 128: 125 us, 0.69 PFLOP/s; 16 heads of 64: 63 us, 0.34; weights and products overlap only in part, and
+// both take some 1000 clocks per 64 keys and 32 rows of 128.
 #include "paged_attn.h"
 
 namespace tsd {
