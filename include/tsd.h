@@ -334,6 +334,72 @@ int tsd_verify_tokens_static(const void* draft_dev, const void* q_dev, const voi
                              const float* uniforms_dev, const int32_t* n_draft_dev, int32_t* n_acc_dev, void* tokens_dev,
                              void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* ---- rounds of drafted trees, windowed caches, scores ------------------------------------------------------------------------
+ * The calls below go with the ones above, under the same terms.  Where drafts form a tree, a round's N new tokens per sequence are its nodes: node 0
+ * the pending token, the others drafted, parents before their children.  A node's cache slot is base + its index, its position base + its depth.  Per layer
+ * tsd_rope_append_static (positions_dev: base + depth) and tsd_tree_attn_static; at the end tsd_verify_tree_static, and tsd_keep_path_static over all
+ * layers, after which the cache holds base + n_acc + 1 tokens in a row. */
+
+/* tsd_paged_attn_static for a model whose tokens see a window: token t of sequence b, at P = lens_dev[b] - n_new + t, sees the keys j <= P with
+ * j > P - window or j < sinks (window >= 1, sinks >= 0).  Pages that no token sees any more may be holes.  What a call costs goes by the
+ * keys that are seen, not by the cache's length.  Otherwise as tsd_paged_attn_static. */
+int tsd_window_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, int32_t window, int32_t sinks,
+                              size_t* bytes_host);
+int tsd_window_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
+                           float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, int32_t max_len, int32_t window, int32_t sinks,
+                           float scale, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* tsd_paged_attn_static where the last n_new tokens of a sequence are the nodes of a tree, or of several: parents_dev int32 [B][T], rows
+ * parents_stride entries apart (0: one tree for all sequences), the index of a node's parent among the new tokens.  An entry that names no earlier node (-1
+ * for one) is none: the node hangs on the tokens before the tree.  Node t sees the keys j < lens_dev[b] - n_new, its ancestors, itself.  With a window
+ * (0: none) and sinks it sees, of these, what tsd_window_attn_static says by positions: a node's is lens_dev[b] - n_new + depth, the depth of
+ * a node without parent 0.  T <= 256 (TSD_E_OUT_OF_RANGE).  Otherwise as tsd_paged_attn_static. */
+int tsd_tree_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, int32_t window, int32_t sinks,
+                            size_t* bytes_host);
+int tsd_tree_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
+                         float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, const int32_t* parents_dev, int32_t parents_stride,
+                         int32_t max_len, int32_t window, int32_t sinks, float scale, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Scores of tokens, from logits (dtype; row t of sequence b at b * stride_b + t * stride_t elements, V of them), softmax at `temperature` (finite, at
+ * least 1e-6), in fp32:
+ *   logprobs_dev float [B][T]: log probability of tokens_dev[b][t] (int32 or int64, token_bytes 4 or 8; both NULL: not asked for), -inf for a
+ *     token outside 0 .. V - 1;
+ *   entropy_dev float [B][T]: -sum p log p, natural logarithms;
+ *   top_ids_dev int32, top_logprobs_dev float [B][T][top] (top 0..32, TSD_E_OUT_OF_RANGE beyond; 0: not asked for): the likeliest tokens, in
+ *     order, of equal logits the lowest index first.  Logits of -inf and NaN are never among them; where fewer are left, -1 and -inf.
+ * n_new_dev int32 [B] (NULL: T each): rows from there on are not read; their numbers are 0, their alternatives -1.  A row without a finite logit
+ * (all -inf): log probabilities -inf, entropy 0; with a NaN or an infinite one: NaN, but for the alternatives' indices.
+ * workspace_dev: tsd_token_logprobs_workspace bytes (often 0), 8-byte aligned, as above.  V <= 2^23. */
+int tsd_token_logprobs_workspace(int32_t B, int32_t T, int32_t V, int32_t top, size_t* bytes_host);
+int tsd_token_logprobs_static(const void* logits_dev, int32_t dtype, int32_t token_bytes, int32_t B, int32_t T, int32_t V, int64_t stride_b,
+                              int64_t stride_t, const void* tokens_dev, const int32_t* n_new_dev, float temperature, int32_t top,
+                              float* logprobs_dev, float* entropy_dev, int32_t* top_ids_dev, float* top_logprobs_dev, void* workspace_dev,
+                              size_t workspace_bytes, void* stream);
+
+/* A tree of drafted tokens against the target's probabilities.  tokens_dev: int32 or int64 (token_bytes 4 or 8) [B][N]; parents_dev int32 [B][N] (rows
+ * parents_stride entries apart, 0: one tree for all): as for tsd_tree_attn_static, node 0 the root whatever its entry says, nodes that do not hang
+ * on it never reached.  p_dev (dtype): row n of sequence b at b * p_stride_b + n * p_stride_n elements, the V probabilities behind node n.
+ * From the root on, step i at node x: a token is drawn from p[x], the first v with p_0 + .. + p_v > u sum(p), u = uniforms_dev[b * N + i] in [0, 1), sums in
+ * 64 bits, weights that are no finite positive number counting as 0 (none left: the token -1).  Where a child of x has it (of several the first) the
+ * walk goes on there; else it ends.  Instead of p_dev and uniforms_dev, choices_dev [B][N] of the tokens' type: the token behind node x is
+ * choices[x], say the likeliest (a negative one ends the walk).
+ *   n_acc_dev int32 [B]: drafted nodes on the way; tokens out_dev [B][N] of the tokens' type: theirs, the last token drawn, -1 behind it;
+ *   path_dev int32 [B][N]: node 0, the nodes on the way, -1 behind them.
+ * n_new_dev int32 [B] (NULL: N each; clamped to 0..N): the nodes that are there; without any n_acc is -1, everything else too.  N <= 256, V <= 2^21
+ * (TSD_E_OUT_OF_RANGE).  workspace_dev: tsd_verify_tree_workspace bytes (often 0; not looked at for choices), 8-byte aligned, as above. */
+int tsd_verify_tree_workspace(int32_t B, int32_t N, int32_t V, int32_t dtype, size_t* bytes_host);
+int tsd_verify_tree_static(const void* tokens_dev, const int32_t* parents_dev, int32_t parents_stride, const void* p_dev, int32_t dtype,
+                           int32_t token_bytes, int32_t B, int32_t N, int32_t V, int64_t p_stride_b, int64_t p_stride_n, const float* uniforms_dev,
+                           const void* choices_dev, const int32_t* n_new_dev, int32_t* n_acc_dev, void* out_dev, int32_t* path_dev,
+                           void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Rolls a cache back to a path through a tree: the keys and values in slot held_dev[b] + path_dev[b][i] go to slot held_dev[b] + i, for i = 0, 1, ..
+ * as long as the path goes up (it ends at an entry that is not above the one before it, is negative, or not below N; tsd_verify_tree_static's ends
+ * at -1).  n_layers caches that lie layer_stride elements apart in both pools, as `cache` describes the first, share the page table.  A token whose
+ * old or new slot is a hole stays where it is, the others move.  Pages that hold what is written must belong to one sequence.  N <= 256. */
+int tsd_keep_path_static(const tsd_paged_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t B, int32_t N, const int32_t* held_dev,
+                         const int32_t* path_dev, void* stream);
+
 /* tsd_draft_propose; tsd_target_verify; tsd_accept_commit(NULL).  On a non-NULL stream that is not
  * being captured by the caller, the launch sequence is captured into a HIP graph on first use and
  * replayed afterwards (same for tsd_target_step); TSD_FLAG_NO_GRAPH switches that off.  Graphs are

@@ -81,6 +81,19 @@ SYMBOLS = {
     "tsd_verify_tokens_workspace": ([C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)], C.c_int),
     "tsd_verify_tokens_static": ([C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int32] * 5 + [C.c_int64] * 4 + [C.c_void_p] * 5
                                  + [C.c_size_t, C.c_void_p], C.c_int),
+    "tsd_window_attn_workspace": ([C.POINTER(TsdPagedCache)] + [C.c_int32] * 6 + [C.POINTER(C.c_size_t)], C.c_int),
+    "tsd_window_attn_static": ([C.POINTER(TsdPagedCache), C.c_int32, C.c_int32, C.c_int32, C.POINTER(TsdRows), C.POINTER(TsdRows), C.c_void_p,
+                                C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p], C.c_int),
+    "tsd_tree_attn_workspace": ([C.POINTER(TsdPagedCache)] + [C.c_int32] * 6 + [C.POINTER(C.c_size_t)], C.c_int),
+    "tsd_tree_attn_static": ([C.POINTER(TsdPagedCache), C.c_int32, C.c_int32, C.c_int32, C.POINTER(TsdRows), C.POINTER(TsdRows)] + [C.c_void_p] * 4
+                             + [C.c_int32] * 4 + [C.c_float, C.c_void_p, C.c_size_t, C.c_void_p], C.c_int),
+    "tsd_token_logprobs_workspace": ([C.c_int32] * 4 + [C.POINTER(C.c_size_t)], C.c_int),
+    "tsd_token_logprobs_static": ([C.c_void_p] + [C.c_int32] * 5 + [C.c_int64] * 2 + [C.c_void_p, C.c_void_p, C.c_float, C.c_int32]
+                                  + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p], C.c_int),
+    "tsd_verify_tree_workspace": ([C.c_int32] * 4 + [C.POINTER(C.c_size_t)], C.c_int),
+    "tsd_verify_tree_static": ([C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p] + [C.c_int32] * 5 + [C.c_int64] * 2 + [C.c_void_p] * 7
+                               + [C.c_size_t, C.c_void_p], C.c_int),
+    "tsd_keep_path_static": ([C.POINTER(TsdPagedCache), C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p], C.c_int),
     "tsd_round": ([C.c_void_p, C.c_void_p], C.c_int),
     "tsd_run_rounds": ([C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p], C.c_int),
     "tsd_target_step": ([C.c_void_p, C.c_void_p], C.c_int),
@@ -107,7 +120,7 @@ SYMBOLS = {
     "tsd_set_sigma": ([C.c_void_p, C.c_float, C.c_float], C.c_int),
 }
 
-_lib = _calls = _round_calls = None
+_lib = _calls = _round_calls = _tree_calls = None
 
 
 def library_path():
@@ -136,7 +149,7 @@ def lib():
 
 def _bind_calls():
     """Load the extension beside the library (building it first only if it does not exist) and hand it the library's entries."""
-    global _calls, _round_calls
+    global _calls, _round_calls, _tree_calls
     handle = lib()
     from . import build as _build
     if not os.path.exists(_build.CALLS):
@@ -149,6 +162,11 @@ def _bind_calls():
             "tsd_rope_append_static", "tsd_paged_attn_workspace", "tsd_paged_attn_static", "tsd_verify_tokens_workspace",
             "tsd_verify_tokens_static")))
         _round_calls = _torch_calls
+    if hasattr(_torch_calls, "bind_trees"):  # (... or those of a round of chains)
+        _torch_calls.bind_trees(*(C.cast(getattr(handle, name), C.c_void_p).value for name in (
+            "tsd_window_attn_workspace", "tsd_window_attn_static", "tsd_tree_attn_workspace", "tsd_tree_attn_static", "tsd_token_logprobs_workspace",
+            "tsd_token_logprobs_static", "tsd_verify_tree_workspace", "tsd_verify_tree_static", "tsd_keep_path_static")))
+        _tree_calls = _torch_calls
     _calls = _torch_calls
 
 
@@ -156,6 +174,13 @@ def _bind_round_calls():
     if _calls is None:
         _bind_calls()
     if _round_calls is None:
+        raise RuntimeError("_torch_calls.so is older than this package: build it again (python -m paper_2511_18191_amd.build)")
+
+
+def _bind_tree_calls():
+    if _calls is None:
+        _bind_calls()
+    if _tree_calls is None:
         raise RuntimeError("_torch_calls.so is older than this package: build it again (python -m paper_2511_18191_amd.build)")
 
 
@@ -247,6 +272,42 @@ def paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len=None, scale=N
     return (out, lse) if want_lse else out
 
 
+def window_attn_static(q, k_pool, v_pool, page_table, lens, window, sinks=0, max_len=None, scale=None, n_new=None, out=None, want_lse=False):
+    """tsd_window_attn_static on torch's current stream of the tensors' device: as paged_attn_static, but a token at position P sees, of the keys up to its
+    own, the last `window` (its own among them) and the first `sinks`.  Pages of page_table that no token sees any more may hold -1."""
+    if _tree_calls is None:
+        _bind_tree_calls()
+    if max_len is not None and max_len < 1:
+        raise ValueError("max_len must be at least 1")
+    if scale is not None and scale != scale:
+        raise ValueError("scale must be finite")
+    rc, out, lse = _tree_calls.window_attn_static(q, k_pool, v_pool, page_table, lens, max_len or 0, float("nan") if scale is None else scale, n_new,
+                                                  out, want_lse, window, sinks)
+    if rc:
+        _check(rc)
+    return (out, lse) if want_lse else out
+
+
+def tree_attn_static(q, k_pool, v_pool, page_table, lens, parents, window=None, sinks=0, max_len=None, scale=None, n_new=None, out=None, want_lse=False):
+    """tsd_tree_attn_static on torch's current stream of the tensors' device: as paged_attn_static, but the last n_new (None: T each) tokens of every
+    sequence are nodes of a tree, each of which sees the tokens before the tree, its ancestors and itself.  parents: int32 [B, T], or [T] for one tree
+    in all sequences: the index of a node's parent, an earlier node; -1 for none.  window (None: all) and sinks as for window_attn_static, by positions: a
+    node's is lens - n_new + its depth.  T is at most 256."""
+    if _tree_calls is None:
+        _bind_tree_calls()
+    if max_len is not None and max_len < 1:
+        raise ValueError("max_len must be at least 1")
+    if window is not None and window < 1:
+        raise ValueError("window must be at least 1")
+    if scale is not None and scale != scale:
+        raise ValueError("scale must be finite")
+    rc, out, lse = _tree_calls.tree_attn_static(q, k_pool, v_pool, page_table, lens, max_len or 0, float("nan") if scale is None else scale, n_new,
+                                                out, want_lse, window or 0, sinks, parents)
+    if rc:
+        _check(rc)
+    return (out, lse) if want_lse else out
+
+
 def verify_tokens_static(draft, q, p, uniforms, n_draft=None):
     """tsd_verify_tokens_static on torch's current stream of the tensors' device.  draft: int32 or int64 [B, K]; q: [B, K, V] or None (certain
     drafts), p: [B, K + 1, V], float32 or bfloat16, rows dense; uniforms: float32 [B, K + 1] in [0, 1), the last of a row for the draw;
@@ -257,6 +318,43 @@ def verify_tokens_static(draft, q, p, uniforms, n_draft=None):
     if rc:
         _check(rc)
     return dict(n_acc=n_acc, tokens=tokens)
+
+
+def token_logprobs_static(logits, tokens=None, top=0, temperature=1.0, n_new=None):
+    """tsd_token_logprobs_static on torch's current stream of the tensors' device.  logits: float32 or bfloat16 [B, T, V], rows dense; tokens: int32 or int64
+    [B, T] or None; n_new: int32 [B] or None, the rows of a sequence that are there.  Returns dict(logprobs float32 [B, T] (None without tokens), entropy float32
+    [B, T], top_ids int32 and top_logprobs float32 [B, T, top] (None without top)).  No gradients, as for rope_append_static."""
+    if _tree_calls is None:
+        _bind_tree_calls()
+    rc, logprobs, entropy, ids, alternatives = _tree_calls.token_logprobs_static(logits, tokens, top, temperature, n_new)
+    if rc:
+        _check(rc)
+    return dict(logprobs=logprobs, entropy=entropy, top_ids=ids, top_logprobs=alternatives)
+
+
+def verify_tree_static(tokens, parents, p=None, uniforms=None, choices=None, n_new=None):
+    """tsd_verify_tree_static on torch's current stream of the tensors' device.  tokens: int32 or int64 [B, N], node 0 the pending token; parents: int32 [B, N] or
+    [N], as for tree_attn_static; either p: [B, N, V] float32 or bfloat16, rows dense, the probabilities behind every node, and uniforms: float32 [B, N] in [0, 1),
+    one a step; or choices: [B, N] of the tokens' type, the token to follow every node; n_new: int32 [B] or None.  Returns dict(n_acc int32 [B], tokens [B, N],
+    path int32 [B, N]): the drafted nodes on the way, their tokens and the one drawn last, the root and these nodes; -1 behind them."""
+    if _tree_calls is None:
+        _bind_tree_calls()
+    rc, n_acc, out, path = _tree_calls.verify_tree_static(tokens, parents, p, uniforms, choices, n_new)
+    if rc:
+        _check(rc)
+    return dict(n_acc=n_acc, tokens=out, path=path)
+
+
+def keep_path_static(k_pool, v_pool, page_table, held, path):
+    """tsd_keep_path_static on torch's current stream of the tensors' device: in every sequence the keys and values of slots held + path[i] move to slots
+    held + i.  Pools as for rope_append_static, or with the layers that share page_table as a first dimension, [layers, pages, page_tokens, kv_heads, head_dim];
+    held: int32 [B], the tokens held before the tree; path: int32 [B, N], as verify_tree_static gives it.  The pools are written in place.  No gradients, as for
+    rope_append_static."""
+    if _tree_calls is None:
+        _bind_tree_calls()
+    rc = _tree_calls.keep_path_static(k_pool, v_pool, page_table, held, path)
+    if rc:
+        _check(rc)
 
 
 def bench_copy(dst, src):

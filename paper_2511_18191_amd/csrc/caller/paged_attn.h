@@ -2,7 +2,7 @@
 // paged_attn_prompt.hip on bf16 caches where rows are many, paged_attn_f32.hip on fp32 ones).
 //
 // Rows: the T new tokens and the G = Hq / Hkv query heads of one key head are rows t * G + g of one product, in tiles, so that a
-// key head's keys and values are read once for all of them.  Row of token t sees keys j < len - n_new + t + 1.
+// key head's keys and values are read once for all of them.  Row of token t sees keys j < len - n_new + t + 1, or fewer of them (AttnMask).
 //
 // Split: the keys of a sequence go in chunks of `chunk`; a workgroup takes one (sequence, key head, row tile, chunk), its wavefronts take
 // its steps of 32 keys in turn, each with a running maximum and sum of its own, joined in LDS at the end.  Where a sequence may
@@ -13,6 +13,15 @@
 #include "paged_cache.h"
 
 namespace tsd {
+
+// Which of the keys up to its own a row sees.
+//   kCausal  all of them;
+//   kWindow  the last `window`, its own among them, and keys 0 .. sinks - 1;
+//   kTree    new tokens are nodes of a tree: the keys before them, its ancestors' and its own; of these, by positions (a node's is
+//            len - n_new + its depth), the last `window` and those below `sinks`.
+// A row tile goes over the keys that some row of it may see only: they are counted through ("places"), the first tokens' and behind them the
+// window's.  Where the window reaches back to the first tokens, or to key 0, places are keys.
+enum AttnMask { kCausal, kWindow, kTree };
 
 struct PagedAttnP {
   PagedView cache;
@@ -27,6 +36,11 @@ struct PagedAttnP {
   float* part_lse;   // [B][splits][T][Hq]
   uint64_t* slots;   // [B][Hkv][row_tiles][splits], or NULL: a second launch joins
   uint64_t tag;
+  int mask;          // AttnMask
+  int window, sinks;   // (kCausal: not looked at)
+  int reach;           // most places a row tile has
+  const int* parents;  // [B or 1][T]
+  int parents_stride;
 };
 
 constexpr int kAttnWaves = 4;  // most wavefronts a workgroup has
@@ -46,13 +60,17 @@ struct AttnWork {
   int row0;           // the tile's first row
   int see_first, see_last;  // keys that the tile's first and last rows see
   int key0, key1;     // this workgroup's keys
+  // kWindow, kTree: where these are places, as is see_first (below it every row sees what its window holds) and
+  int first, gap;     // place v is key v, from `first` on v + gap
+  int low_last;       // from here on every row's window holds what comes
+  int held;           // place of the first new token
   bool split_out;     // its rows' sums go to the workspace
   bool idle;          // no rows or no chunk: nothing to write
 };
 
 // Chunks of a sequence that hold keys (at least one, which then writes the empty rows).
 __device__ __forceinline__ int attn_chunks(const PagedAttnP& p, int len) {
-  return min(p.splits, max(1, (len + p.chunk - 1) / p.chunk));
+  return min(p.splits, max(1, (min(len, p.reach) + p.chunk - 1) / p.chunk));
 }
 
 __device__ __forceinline__ int attn_len(const PagedAttnP& p, int b) { return min(max(p.lens[b], 0), 1 << 30); }
@@ -78,6 +96,7 @@ __device__ __forceinline__ AttnWork attn_place(const PagedAttnP& p, int tile_row
   w.split_out = p.splits > 1;
   return w;
 }
+template <int M>
 __device__ __forceinline__ void attn_lengths(const PagedAttnP& p, AttnWork& w, int tile_rows) {
   w.len = attn_len(p, w.b);
   w.n_new = attn_new(p, w.b);
@@ -86,7 +105,20 @@ __device__ __forceinline__ void attn_lengths(const PagedAttnP& p, AttnWork& w, i
   w.idle = w.row0 >= w.rows || w.split >= chunks;
   w.see_first = w.len - w.n_new + w.row0 / p.G + 1;
   w.see_last = w.len - w.n_new + (min(w.rows, w.row0 + tile_rows) - 1) / p.G + 1;
-  const int end = min(w.see_last, p.cache.cols << p.cache.pt_shift);
+  int end = min(w.see_last, p.cache.cols << p.cache.pt_shift);
+  if constexpr (M != kCausal) {
+    w.held = w.len - w.n_new;
+    // (a node's position is its token's or less)
+    const int nearest = M == kTree ? w.held : w.see_first - 1, furthest = M == kTree ? w.len - 1 : w.see_last - 1;
+    const int lo = max(nearest - p.window + 1, 0);
+    w.first = min(p.sinks, lo);
+    w.gap = lo - w.first;
+    w.low_last = max(furthest - p.window + 1, 0) - w.gap;
+    w.held -= w.gap;
+    w.see_first = M == kTree ? w.held : w.see_first - w.gap;
+    w.see_last -= w.gap;
+    end = min(w.see_last, max(w.first, (p.cache.cols << p.cache.pt_shift) - w.gap));
+  }
   // (the last chunk of the grid takes what is left, so that a length beyond max_len is slow and not wrong)
   w.key1 = w.split == chunks - 1 ? end : min(end, w.key0 + p.chunk);
 }
@@ -96,9 +128,123 @@ __device__ __forceinline__ int attn_sees(const PagedAttnP& p, const AttnWork& w,
   return row < w.rows ? w.len - w.n_new + row / p.G + 1 : 0;
 }
 
-// Offset of the cache row of key `key`, whose table entry is given, or -1 (see paged_row).
-__device__ __forceinline__ long attn_key_row(const PagedAttnP& p, const AttnWork& w, int entry, int key) {
-  return key < w.key1 ? paged_row(p.cache, entry, key) : -1;
+// What a row sees: places below `sees`, of these from `low` on or below p.sinks; of kTree's nodes those of its line (bit i: node i).
+struct AttnSight {
+  int sees, low;
+  const uint64_t* line;
+};
+template <int M>
+__device__ __forceinline__ AttnSight attn_sight(const PagedAttnP& p, const AttnWork& w, int row) {
+  AttnSight a;
+  a.sees = attn_sees(p, w, row) - (M == kCausal ? 0 : w.gap);
+  a.low = max(a.sees - p.window, 0);
+  if (M == kWindow && row >= w.rows) a.sees = 0;
+  a.line = nullptr;
+  return a;
+}
+
+// The first n of 32 bits.
+__device__ __forceinline__ unsigned attn_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+// Bits k .. k + 31 of a line.
+__device__ __forceinline__ unsigned attn_line_bits(const uint64_t* line, int k) {
+  if (k <= -32 || k >= kTreeNodes) return 0u;
+  if (k < 0) return (unsigned)(line[0] << -k);
+  const int i = k >> 6, s = k & 63;
+  uint64_t x = line[i] >> s;
+  if (s > 32 && i + 1 < kTreeNodes / 64) x |= line[i + 1] << (64 - s);
+  return (unsigned)x;
+}
+
+// Which of the places sb .. sb + 31 a row sees.
+template <int M>
+__device__ __forceinline__ unsigned attn_seen(const PagedAttnP& p, const AttnWork& w, const AttnSight& a, int sb) {
+  unsigned x = attn_bits(a.sees - sb) & (~attn_bits(a.low - sb) | attn_bits(p.sinks - sb));
+  if (M == kTree) x |= attn_line_bits(a.line, sb - w.held);
+  return x;
+}
+
+// Whether every row of the tile sees all of the places sb .. sb + step - 1 that hold keys.
+template <int M>
+__device__ __forceinline__ bool attn_all_see(const PagedAttnP& p, const AttnWork& w, int sb, int step) {
+  return sb + step <= w.see_first && (M == kCausal || sb >= w.low_last || sb + step <= p.sinks);
+}
+// Whether rows differ in what they see of them.
+template <int M>
+__device__ __forceinline__ bool attn_mixed(const PagedAttnP& p, const AttnWork& w, int sb, int step) {
+  return w.see_first < w.see_last && !attn_all_see<M>(p, w, sb, step);
+}
+
+// The key at a place.
+template <int M>
+__device__ __forceinline__ int attn_key(const AttnWork& w, int place) {
+  return M == kCausal ? place : place + (place >= w.first ? w.gap : 0);
+}
+template <int M>
+__device__ __forceinline__ int attn_entry(const PagedAttnP& p, const AttnWork& w, const int* table, int place) {
+  return paged_entry(p.cache, table, attn_key<M>(w, place));
+}
+// Offset of the cache row of the key at a place, whose table entry is given, or -1 (see paged_row).
+template <int M>
+__device__ __forceinline__ long attn_key_row(const PagedAttnP& p, const AttnWork& w, int entry, int place) {
+  return place < w.key1 ? paged_row(p.cache, entry, attn_key<M>(w, place)) : -1;
+}
+
+// The parents of a sequence's nodes into LDS, -1 where an entry names no earlier node.  For a whole workgroup, which waits.
+__device__ __forceinline__ void attn_parents(const PagedAttnP& p, const AttnWork& w, short* parents) {
+  for (int i = threadIdx.x; i < w.n_new; i += blockDim.x) {
+    const int x = p.parents[(long)w.b * p.parents_stride + i];
+    parents[i] = (unsigned)x < (unsigned)i ? (short)x : (short)-1;
+  }
+  __syncthreads();
+}
+// A node's line: itself and those of its ancestors that it sees.  Returns its depth.  (Parents come before their children: it ends.)
+__device__ __forceinline__ int attn_line(const PagedAttnP& p, const AttnWork& w, const short* parents, int node, uint64_t (&line)[kTreeNodes / 64]) {
+  constexpr int N = kTreeNodes / 64;
+#pragma unroll
+  for (int i = 0; i < N; ++i) line[i] = 0;
+  int depth = -1;
+  for (int a = node; a >= 0; a = parents[a]) {
+    ++depth;
+#pragma unroll
+    for (int i = 0; i < N; ++i) line[i] |= a >> 6 == i ? 1ull << (a & 63) : 0ull;
+  }
+  if (depth < p.window) return depth;
+  int at = depth;
+  for (int a = node; a >= 0; a = parents[a], --at)
+    if (at <= depth - p.window && w.len - w.n_new + at >= p.sinks) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) line[i] &= ~(a >> 6 == i ? 1ull << (a & 63) : 0ull);
+    }
+  return depth;
+}
+// What the row of a node of this line and depth sees.
+__device__ __forceinline__ AttnSight attn_node_sight(const PagedAttnP& p, const AttnWork& w, int depth, const uint64_t* line) {
+  return {max(w.held, 0), max(w.held + depth - p.window + 1, 0), line};
+}
+
+// kTree: lines and depths of a tile's tokens in LDS.  For a whole workgroup, which waits; tokens: w.row0 / G on, at most kLineTokens.
+constexpr int kLineTokens = 32;
+struct AttnLines {
+  uint64_t line[kLineTokens + 1][kTreeNodes / 64];  // (the last: of rows that are not there)
+  short parents[kTreeNodes];
+  short depth[kLineTokens + 1];
+};
+__device__ __forceinline__ void attn_lines(const PagedAttnP& p, const AttnWork& w, int tile_rows, AttnLines& l) {
+  attn_parents(p, w, l.parents);
+  const int t0 = w.row0 / p.G, n = (min(w.rows, w.row0 + tile_rows) - 1) / p.G - t0 + 1;
+  for (int i = threadIdx.x; i <= kLineTokens; i += blockDim.x) {
+    uint64_t line[kTreeNodes / 64] = {};
+    l.depth[i] = i < n ? (short)attn_line(p, w, l.parents, t0 + i, line) : (short)0;
+#pragma unroll
+    for (int j = 0; j < kTreeNodes / 64; ++j) l.line[i][j] = line[j];
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ AttnSight attn_tree_sight(const PagedAttnP& p, const AttnWork& w, const AttnLines& l, int row) {
+  if (row >= w.rows) return {0, 0, l.line[kLineTokens]};
+  const int i = row / p.G - w.row0 / p.G;
+  return attn_node_sight(p, w, l.depth[i], l.line[i]);
 }
 
 // One step of the running softmax of a row: its lanes (q, q + 16, q + 32, q + 48) hold 8 scores each, in base 2 and -inf where the row does not
@@ -146,8 +292,11 @@ __device__ __forceinline__ bool attn_take_out(f32x4& v) {
 // What of `v` was taken out.
 __device__ __forceinline__ float attn_taken(float v) { return (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? v : 0.f; }
 
-// The first key of the mixed steps of `step` keys.
-__device__ __forceinline__ int attn_mixed_from(const AttnWork& w, int step) { return w.key0 + max(w.see_first - w.key0, 0) / step * step; }
+// The first key of the mixed steps of `step` keys (but for kCausal there may be others among them that are not).
+template <int M>
+__device__ __forceinline__ int attn_mixed_from(const AttnWork& w, int step) {
+  return M == kCausal ? w.key0 + max(w.see_first - w.key0, 0) / step * step : w.key0;
+}
 
 // Writes dims d .. d + 3 of a row of the output.
 template <typename T>

@@ -22,7 +22,7 @@ namespace {
 
 constexpr int v_stride(int dp) { return dp + 16; }  // V row in LDS: 32 bytes more than its dims, so that 8 rows fall on different banks
 
-template <int DP, int MT, bool FULL>  // FULL: head_dim is DP
+template <int M, int DP, int MT, bool FULL>  // M: AttnMask; FULL: head_dim is DP
 __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn_bf16_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int KK = DP / 32, NB = DP / 16, VS = v_stride(DP), NV = DP / 16, VC = DP / 8;
@@ -33,20 +33,36 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
   const int stride = 32 * waves;
   int sb = w.key0 + 32 * wave;
   // (lane i and lane i + 32: key i of a step)
-  int entry = paged_entry(p.cache, table, sb + (lane & 31)), next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
-  attn_lengths(p, w, 16 * MT);
+  int entry, next_entry;
+  if constexpr (M == kCausal) {  // (the table's entries are on their way before the lengths are there)
+    entry = paged_entry(p.cache, table, sb + (lane & 31));
+    next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
+  }
+  attn_lengths<M>(p, w, 16 * MT);
   if (w.idle) return;
+  if constexpr (M != kCausal) {
+    entry = attn_entry<M>(p, w, table, sb + (lane & 31));
+    next_entry = attn_entry<M>(p, w, table, sb + stride + (lane & 31));
+  }
+  __shared__ std::conditional_t<M == kTree, AttnLines, int> lines;
+  if constexpr (M == kTree) attn_lines(p, w, 16 * MT, lines);
+  const auto sight = [&](int row) {
+    if constexpr (M == kTree)
+      return attn_tree_sight(p, w, lines, row);
+    else
+      return attn_sight<M>(p, w, row);
+  };
   const bf16* kbase = reinterpret_cast<const bf16*>(p.cache.k) + w.hk * p.cache.head_stride;
   const bf16* vbase = reinterpret_cast<const bf16*>(p.cache.v) + w.hk * p.cache.head_stride;
   bf16* vt = reinterpret_cast<bf16*>(smem) + wave * 32 * VS;
   const bf16x8 zero = {};
 
   bf16x8 qf[MT][KK];
-  int sees[MT];
+  AttnSight sees[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int row = w.row0 + mt * 16 + qi;
-    sees[mt] = attn_sees(p, w, row);
+    sees[mt] = sight(row);
     const int r = min(row, w.rows - 1), t = r / p.G, h = w.hk * p.G + r - t * p.G;
     const bf16* q = reinterpret_cast<const bf16*>(p.q.p) + w.b * p.q.sb + t * p.q.st + h * p.q.sh;
 #pragma unroll
@@ -93,7 +109,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
     }
   };
 
-  long off = attn_key_row(p, w, entry, sb + (lane & 31));
+  long off = attn_key_row<M>(p, w, entry, sb + (lane & 31));
   entry = next_entry;
   unsigned valid = (unsigned)__ballot(off >= 0), next_valid = 0;
   if (sb < w.key1) {
@@ -101,8 +117,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
     load_k(off);
     load_v(off);
   }
-  off = attn_key_row(p, w, entry, sb + stride + (lane & 31));
-  entry = paged_entry(p.cache, table, sb + 2 * stride + (lane & 31));
+  off = attn_key_row<M>(p, w, entry, sb + stride + (lane & 31));
+  entry = attn_entry<M>(p, w, table, sb + 2 * stride + (lane & 31));
   bool odd = false;
   for (; sb < w.key1; sb += stride, valid = next_valid) {
     const bool more = sb + stride < w.key1;
@@ -110,15 +126,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
     off = max(off, 0l);
     // (the entries of the step after the next are read before loads are issued that nothing waits for yet: counted waits do not
     // survive the branches between)
-    const long later = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
-    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
-    const bool whole = valid == 0xFFFFFFFFu && sb + 32 <= w.see_first;  // every row of the tile sees every key
+    const long later = attn_key_row<M>(p, w, entry, sb + 2 * stride + (lane & 31));
+    entry = attn_entry<M>(p, w, table, sb + 3 * stride + (lane & 31));
+    const bool whole = valid == 0xFFFFFFFFu && attn_all_see<M>(p, w, sb, 32);  // every row of the tile sees every key
     if (!whole) {
       // keys that are not there hold anything; their weights are 0, and so must the values be
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (!(valid >> ((i * 64 + lane) / VC) & 1)) vf[i] = zero;
-      if (w.see_first < w.see_last && sb + 32 > w.see_first) {
+      if (attn_mixed<M>(p, w, sb, 32)) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) odd |= attn_take_out(vf[i]);
       }
@@ -150,10 +166,10 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] = sc[mt][j >> 2][j & 3] * p.scale2;
       if (!whole) {
-        const unsigned live = valid >> (8 * g);
+        const unsigned live = (M == kCausal ? valid : valid & attn_seen<M>(p, w, sees[mt], sb)) >> (8 * g);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (!(live >> j & 1) || sb + 8 * g + j >= sees[mt]) s[j] = -INFINITY;
+          if (!(live >> j & 1) || (M == kCausal && sb + 8 * g + j >= sees[mt].sees)) s[j] = -INFINITY;
       }
       const float alpha = attn_running_max(s, m_run[mt], e);
       float sum = 0.f;
@@ -188,9 +204,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
     }
   }
   if (__any(odd)) {
-    for (int key = attn_mixed_from(w, 32); key < w.key1; ++key) {
-      const long at = attn_key_row(p, w, paged_entry(p.cache, table, key), key);
-      if (at < 0 || (key - w.key0) / 32 % waves != wave) continue;
+    const auto reaches = [&](int key, int mt, int r) {
+      if constexpr (M == kCausal)
+        return key < __shfl(sees[mt].sees, 4 * g + r);
+      else
+        return bool(attn_seen<M>(p, w, sight(w.row0 + mt * 16 + 4 * g + r), key) & 1);
+    };
+    for (int key = attn_mixed_from<M>(w, 32); key < w.key1; ++key) {
+      const long at = attn_key_row<M>(p, w, attn_entry<M>(p, w, table, key), key);
+      if (at < 0 || (key - w.key0) / 32 % waves != wave || (M != kCausal && !attn_mixed<M>(p, w, key - (key - w.key0) % 32, 32))) continue;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const float v = FULL || nb * 16 + qi < p.D ? attn_taken((float)vbase[at + nb * 16 + qi]) : 0.f;
@@ -198,7 +220,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (key < __shfl(sees[mt], 4 * g + r)) o[mt][nb][r] += v;
+            if (reaches(key, mt, r)) o[mt][nb][r] += v;
       }
     }
   }
@@ -288,16 +310,16 @@ hipError_t launch_join(const PagedAttnP& p, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int DP>
+template <int M, int DP>
 hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
   const dim3 grid((unsigned)((long)p.B * p.Hkv * p.row_tiles * p.splits));
   const size_t stage = (size_t)waves * 32 * v_stride(DP) * 2, join = (size_t)waves * 16 * ((DP + 4) * 4 + 8);
   const size_t lds = stage > join ? stage : join;
   const auto go = [&](auto kernel) { kernel<<<grid, waves * 64, lds, st>>>(p); };
   if (mt == 1)
-    go(p.D == DP ? paged_attn_bf16_kernel<DP, 1, true> : paged_attn_bf16_kernel<DP, 1, false>);
+    go(p.D == DP ? paged_attn_bf16_kernel<M, DP, 1, true> : paged_attn_bf16_kernel<M, DP, 1, false>);
   else if constexpr (DP <= 128)
-    go(p.D == DP ? paged_attn_bf16_kernel<DP, 2, true> : paged_attn_bf16_kernel<DP, 2, false>);
+    go(p.D == DP ? paged_attn_bf16_kernel<M, DP, 2, true> : paged_attn_bf16_kernel<M, DP, 2, false>);
   return hipGetLastError();
 }
 
@@ -319,19 +341,34 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3), and not for many rows (2 chunks of 128 rows of 64 24.5 and 15.4).
 // Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys
 // 45.9 us, two 46.8, four 52.0).
+// All of this goes by the places that a row tile may have, where windows leave fewer of them than max_len.
 struct AttnPlan {
   bool prompt;  // the kernel for many rows
-  int mt, waves, row_tiles, splits, chunk;
+  int mt, waves, row_tiles, splits, chunk, reach;
   bool joins;   // the last workgroup of a tile joins its chunks
 };
 
-AttnPlan attn_plan(int dtype, int B, int T, int Hq, int Hkv, int D, int max_len) {
+// What a call says of its mask.
+struct AttnAsk {
+  AttnMask mask;
+  int window, sinks;
+  const int32_t* parents;
+  int parents_stride;
+};
+constexpr int kMostTokens = 1 << 30;
+constexpr AttnAsk kAllKeys = {kCausal, kMostTokens, 0, nullptr, 0};
+
+AttnPlan attn_plan(const AttnAsk& ask, int dtype, int B, int T, int Hq, int Hkv, int D, int max_len) {
   AttnPlan a;
   const int64_t rows = (int64_t)T * (Hq / Hkv);
   a.prompt = dtype == TSD_BF16 && D <= 128 && (rows > 64 || (rows > 32 && D > 96 && (int64_t)B * Hkv >= 64));
   a.mt = rows <= 16 || D > 128 ? 1 : 2;
   const int tile_rows = a.prompt ? kPromptRows : 16 * a.mt;
   a.row_tiles = (int)((rows + tile_rows - 1) / tile_rows);
+  // (the tokens that a tile's rows may belong to; a tree's nodes are at most as far apart as there are nodes)
+  const int64_t tokens = ask.mask == kTree ? T : std::min<int64_t>(T, (tile_rows + Hq / Hkv - 2) / (Hq / Hkv) + 1);
+  a.reach = (int)std::min<int64_t>(kMostTokens, (int64_t)ask.sinks + ask.window + tokens - 1);
+  max_len = std::min(max_len, a.reach);
   const int64_t base = (int64_t)B * Hkv * a.row_tiles, steps = (max_len + 31) / 32;  // workgroups where nothing is split
   a.waves = a.prompt ? kPromptWaves : (int)std::min<int64_t>(base >= 1024 && steps <= 4 ? 1 : D > 128 ? 2 : kAttnWaves, steps);
   const int64_t step = a.prompt ? 64 : 32 * a.waves;
@@ -356,7 +393,7 @@ int check_attn(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_h
   if (rc) return rc;
   if (n_q_heads < 1 || n_q_heads > 1024 || n_q_heads % cache->n_kv_heads)
     return fail_no_handle(TSD_E_INVALID_ARG, "n_q_heads must be a multiple of n_kv_heads, at most 1024");
-  if (max_len < 1 || max_len > (1 << 30)) return fail_no_handle(TSD_E_INVALID_ARG, "max_len must be 1..2^30");
+  if (max_len < 1 || max_len > kMostTokens) return fail_no_handle(TSD_E_INVALID_ARG, "max_len must be 1..2^30");
   if ((int64_t)B * T * n_q_heads > INT32_MAX) return fail_no_handle(TSD_E_OUT_OF_RANGE, "B * T * n_q_heads beyond 2^31 - 1");
   return TSD_OK;
 }
@@ -368,41 +405,60 @@ size_t attn_bytes(const AttnPlan& a, int B, int T, int Hq, int Hkv, int D) {
   return (attn_part_bytes(a, B, T, Hq, D) + (size_t)B * Hkv * a.row_tiles * a.splits * 8 + 255) / 256 * 256;
 }
 
+template <int M>
+hipError_t launch_mask(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
+  if (p.D <= 32) return launch_dp<M, 32>(p, mt, waves, st);
+  if (p.D <= 64) return launch_dp<M, 64>(p, mt, waves, st);
+  if (p.D <= 96) return launch_dp<M, 96>(p, mt, waves, st);
+  if (p.D <= 128) return launch_dp<M, 128>(p, mt, waves, st);
+  return launch_dp<M, 256>(p, mt, waves, st);
+}
+
 }  // namespace
 
 hipError_t launch_paged_attn_bf16(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
-  if (p.D <= 32) return launch_dp<32>(p, mt, waves, st);
-  if (p.D <= 64) return launch_dp<64>(p, mt, waves, st);
-  if (p.D <= 96) return launch_dp<96>(p, mt, waves, st);
-  if (p.D <= 128) return launch_dp<128>(p, mt, waves, st);
-  return launch_dp<256>(p, mt, waves, st);
+  return p.mask == kCausal ? launch_mask<kCausal>(p, mt, waves, st) : p.mask == kWindow ? launch_mask<kWindow>(p, mt, waves, st) : launch_mask<kTree>(p, mt, waves, st);
 }
 
 }  // namespace tsd
 
 using namespace tsd;
 
-extern "C" int tsd_paged_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, size_t* bytes_host) {
-  const int rc = check_attn(cache, B, T, n_q_heads, max_len);
-  if (rc) return rc;
-  if (!bytes_host) return fail_no_handle(TSD_E_INVALID_ARG, "bytes_host must not be NULL");
-  *bytes_host = attn_bytes(attn_plan(cache->dtype, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim, max_len), B, T, n_q_heads, cache->n_kv_heads, cache->head_dim);
+namespace {
+
+// A window of 0: every key before a row's own.
+int check_ask(const AttnAsk& ask, int32_t T) {
+  if (ask.mask == kCausal) return TSD_OK;
+  if (ask.window < 1) return fail_no_handle(TSD_E_INVALID_ARG, ask.mask == kTree ? "window must not be negative" : "window must be at least 1");
+  if (ask.sinks < 0) return fail_no_handle(TSD_E_INVALID_ARG, "sinks must not be negative");
+  if (ask.mask == kTree && T > kTreeNodes) return fail_no_handle(TSD_E_OUT_OF_RANGE, "a tree has at most 256 nodes");
   return TSD_OK;
 }
 
-extern "C" int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
-                                     float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, int32_t max_len, float scale,
-                                     void* workspace_dev, size_t workspace_bytes, void* stream) {
+int attn_workspace(const AttnAsk& ask, const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, size_t* bytes_host) {
   int rc = check_attn(cache, B, T, n_q_heads, max_len);
-  if (rc) return rc;
+  if (rc || (rc = check_ask(ask, T))) return rc;
+  if (!bytes_host) return fail_no_handle(TSD_E_INVALID_ARG, "bytes_host must not be NULL");
+  const AttnPlan a = attn_plan(ask, cache->dtype, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim, max_len);
+  *bytes_host = attn_bytes(a, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim);
+  return TSD_OK;
+}
+
+int attn_call(const AttnAsk& ask, const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
+              float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, int32_t max_len, float scale, void* workspace_dev,
+              size_t workspace_bytes, void* stream) {
+  int rc = check_attn(cache, B, T, n_q_heads, max_len);
+  if (rc || (rc = check_ask(ask, T))) return rc;
   const int es = type_bytes(cache->dtype);
   if ((rc = check_rows(q, es, "q")) || (rc = check_rows(out, es, "out"))) return rc;
   if (!lens_dev) return fail_no_handle(TSD_E_INVALID_ARG, "lens_dev must not be NULL");
+  if (ask.mask == kTree && !ask.parents) return fail_no_handle(TSD_E_INVALID_ARG, "parents_dev must not be NULL");
+  if (ask.mask == kTree && ask.parents_stride && ask.parents_stride < T) return fail_no_handle(TSD_E_INVALID_ARG, "parents_stride must be 0 or at least T");
   if (!std::isfinite(scale)) return fail_no_handle(TSD_E_INVALID_ARG, "scale must be finite");
-  const AttnPlan a = attn_plan(cache->dtype, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim, max_len);
+  const AttnPlan a = attn_plan(ask, cache->dtype, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim, max_len);
   const size_t need = attn_bytes(a, B, T, n_q_heads, cache->n_kv_heads, cache->head_dim);
   if (need && (!workspace_dev || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
-    return fail_no_handle(TSD_E_INVALID_ARG, "workspace: needs the bytes that tsd_paged_attn_workspace gives for these sizes, 16-byte aligned");
+    return fail_no_handle(TSD_E_INVALID_ARG, "workspace: needs the bytes that the call for its size gives for these sizes, 16-byte aligned");
   if ((int64_t)B * cache->n_kv_heads * a.row_tiles * a.splits > max_workgroups(64 * kAttnWaves) ||
       (a.splits > 1 && (int64_t)B * T * n_q_heads > max_workgroups(256)))
     return fail_no_handle(TSD_E_OUT_OF_RANGE, "more than 2^24 - 1 workgroups");
@@ -427,10 +483,58 @@ extern "C" int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, in
   p.part_lse = need ? p.part_o + (size_t)B * a.splits * T * n_q_heads * cache->head_dim : nullptr;
   p.slots = a.joins ? reinterpret_cast<uint64_t*>(static_cast<char*>(workspace_dev) + attn_part_bytes(a, B, T, n_q_heads, cache->head_dim)) : nullptr;
   p.tag = a.joins ? new_tag() : 0;
+  p.mask = ask.mask;
+  p.window = ask.window;
+  p.sinks = ask.sinks;
+  p.reach = a.reach;
+  p.parents = ask.parents;
+  p.parents_stride = ask.parents_stride;
   const hipStream_t st = (hipStream_t)stream;
   hipError_t e = a.prompt                   ? launch_paged_attn_prompt(p, st)
                  : cache->dtype == TSD_BF16 ? launch_paged_attn_bf16(p, a.mt, a.waves, st)
                                             : launch_paged_attn_f32(p, a.mt, a.waves, st);
   if (e == hipSuccess && a.splits > 1 && !a.joins) e = cache->dtype == TSD_BF16 ? launch_join<bf16>(p, st) : launch_join<float>(p, st);
   return e == hipSuccess ? TSD_OK : fail_no_handle(TSD_E_HIP, std::string("paged attention launch: ") + hipGetErrorString(e));
+}
+
+AttnAsk window_ask(int32_t window, int32_t sinks) { return {kWindow, std::min<int>(window, kMostTokens), std::min<int>(sinks, kMostTokens), nullptr, 0}; }
+AttnAsk tree_ask(int32_t window, int32_t sinks, const int32_t* parents, int32_t stride) {
+  return {kTree, window ? std::min<int>(window, kMostTokens) : kMostTokens, std::min<int>(sinks, kMostTokens), parents, stride};
+}
+
+}  // namespace
+
+extern "C" int tsd_paged_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, size_t* bytes_host) {
+  return attn_workspace(kAllKeys, cache, B, T, n_q_heads, max_len, bytes_host);
+}
+
+extern "C" int tsd_paged_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
+                                     float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, int32_t max_len, float scale,
+                                     void* workspace_dev, size_t workspace_bytes, void* stream) {
+  return attn_call(kAllKeys, cache, B, T, n_q_heads, q, out, lse_dev, lens_dev, n_new_dev, max_len, scale, workspace_dev, workspace_bytes, stream);
+}
+
+extern "C" int tsd_window_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, int32_t window,
+                                         int32_t sinks, size_t* bytes_host) {
+  return attn_workspace(window_ask(window, sinks), cache, B, T, n_q_heads, max_len, bytes_host);
+}
+
+extern "C" int tsd_window_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
+                                      float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, int32_t max_len, int32_t window,
+                                      int32_t sinks, float scale, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  return attn_call(window_ask(window, sinks), cache, B, T, n_q_heads, q, out, lse_dev, lens_dev, n_new_dev, max_len, scale, workspace_dev,
+                   workspace_bytes, stream);
+}
+
+extern "C" int tsd_tree_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, int32_t window,
+                                       int32_t sinks, size_t* bytes_host) {
+  return attn_workspace(tree_ask(window, sinks, nullptr, 0), cache, B, T, n_q_heads, max_len, bytes_host);
+}
+
+extern "C" int tsd_tree_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,
+                                    float* lse_dev, const int32_t* lens_dev, const int32_t* n_new_dev, const int32_t* parents_dev,
+                                    int32_t parents_stride, int32_t max_len, int32_t window, int32_t sinks, float scale, void* workspace_dev,
+                                    size_t workspace_bytes, void* stream) {
+  return attn_call(tree_ask(window, sinks, parents_dev, parents_stride), cache, B, T, n_q_heads, q, out, lse_dev, lens_dev, n_new_dev, max_len,
+                   scale, workspace_dev, workspace_bytes, stream);
 }

@@ -12,7 +12,7 @@
 namespace tsd {
 namespace {
 
-template <int DP, int MT, bool FULL>  // FULL: head_dim is DP
+template <int M, int DP, int MT, bool FULL>  // M: AttnMask; FULL: head_dim is DP
 __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_f32_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int KC = DP / 16, NC = DP / 64;
@@ -23,19 +23,35 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
   const int stride = 32 * waves;
   int sb = w.key0 + 32 * wave;
   // (lane i and lane i + 32: key i of a step)
-  int entry = paged_entry(p.cache, table, sb + (lane & 31)), next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
-  attn_lengths(p, w, 16 * MT);
+  int entry, next_entry;
+  if constexpr (M == kCausal) {  // (the table's entries are on their way before the lengths are there)
+    entry = paged_entry(p.cache, table, sb + (lane & 31));
+    next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
+  }
+  attn_lengths<M>(p, w, 16 * MT);
   if (w.idle) return;
+  if constexpr (M != kCausal) {
+    entry = attn_entry<M>(p, w, table, sb + (lane & 31));
+    next_entry = attn_entry<M>(p, w, table, sb + stride + (lane & 31));
+  }
+  __shared__ std::conditional_t<M == kTree, AttnLines, int> lines;
+  if constexpr (M == kTree) attn_lines(p, w, 16 * MT, lines);
+  const auto sight = [&](int row) {
+    if constexpr (M == kTree)
+      return attn_tree_sight(p, w, lines, row);
+    else
+      return attn_sight<M>(p, w, row);
+  };
   const float* kbase = reinterpret_cast<const float*>(p.cache.k) + w.hk * p.cache.head_stride;
   const float* vbase = reinterpret_cast<const float*>(p.cache.v) + w.hk * p.cache.head_stride;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
   f32x4 qf[MT][KC];
-  int sees[MT];
+  AttnSight sees[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int row = w.row0 + mt * 16 + qi;
-    sees[mt] = attn_sees(p, w, row);
+    sees[mt] = sight(row);
     const int r = min(row, w.rows - 1), t = r / p.G, h = w.hk * p.G + r - t * p.G;
     const float* q = reinterpret_cast<const float*>(p.q.p) + w.b * p.q.sb + t * p.q.st + h * p.q.sh;
 #pragma unroll
@@ -77,7 +93,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
       }
   };
 
-  long off = attn_key_row(p, w, entry, sb + (lane & 31));
+  long off = attn_key_row<M>(p, w, entry, sb + (lane & 31));
   entry = next_entry;
   unsigned valid = (unsigned)__ballot(off >= 0), next_valid = 0;
   if (sb < w.key1) {
@@ -85,8 +101,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
     load_k(off);
     load_v(off);
   }
-  off = attn_key_row(p, w, entry, sb + stride + (lane & 31));
-  entry = paged_entry(p.cache, table, sb + 2 * stride + (lane & 31));
+  off = attn_key_row<M>(p, w, entry, sb + stride + (lane & 31));
+  entry = attn_entry<M>(p, w, table, sb + 2 * stride + (lane & 31));
   bool odd = false;
   for (; sb < w.key1; sb += stride, valid = next_valid) {
     const bool more = sb + stride < w.key1;
@@ -94,9 +110,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
     off = max(off, 0l);
     // (the entries of the step after the next are read before loads are issued that nothing waits for yet: counted waits do not
     // survive the branches between)
-    const long later = attn_key_row(p, w, entry, sb + 2 * stride + (lane & 31));
-    entry = paged_entry(p.cache, table, sb + 3 * stride + (lane & 31));
-    const bool whole = valid == 0xFFFFFFFFu && sb + 32 <= w.see_first;
+    const long later = attn_key_row<M>(p, w, entry, sb + 2 * stride + (lane & 31));
+    entry = attn_entry<M>(p, w, table, sb + 3 * stride + (lane & 31));
+    const bool whole = valid == 0xFFFFFFFFu && attn_all_see<M>(p, w, sb, 32);
     f32x4 sc[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -110,7 +126,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
       }
     if (more) load_k(off);
     if (!whole) {
-      const bool mixed = w.see_first < w.see_last && sb + 32 > w.see_first;  // (see attn_take_out)
+      const bool mixed = attn_mixed<M>(p, w, sb, 32);  // (see attn_take_out)
 #pragma unroll
       for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
@@ -125,11 +141,12 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float s[8];
+      const unsigned live = M == kCausal || whole ? valid : valid & attn_seen<M>(p, w, sees[mt], sb);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s[j] = sc[mt][j >> 2][j & 3] * p.scale2;
         const int key = 16 * (j >> 2) + 4 * g + (j & 3);
-        if (!whole && (!(valid >> key & 1) || sb + key >= sees[mt])) s[j] = -INFINITY;
+        if (!whole && (!(live >> key & 1) || (M == kCausal && sb + key >= sees[mt].sees))) s[j] = -INFINITY;
       }
       const float alpha = attn_running_max(s, m_run[mt], e[mt]);
       float sum = 0.f;
@@ -163,9 +180,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
   }
 
   if (__any(odd)) {
-    for (int key = attn_mixed_from(w, 32); key < w.key1; ++key) {
-      const long at = attn_key_row(p, w, paged_entry(p.cache, table, key), key);
-      if (at < 0 || (key - w.key0) / 32 % waves != wave) continue;
+    const auto reaches = [&](int key, int mt, int r) {
+      if constexpr (M == kCausal)
+        return key < __shfl(sees[mt].sees, 4 * g + r);
+      else
+        return bool(attn_seen<M>(p, w, sight(w.row0 + mt * 16 + 4 * g + r), key) & 1);
+    };
+    for (int key = attn_mixed_from<M>(w, 32); key < w.key1; ++key) {
+      const long at = attn_key_row<M>(p, w, attn_entry<M>(p, w, table, key), key);
+      if (at < 0 || (key - w.key0) / 32 % waves != wave || (M != kCausal && !attn_mixed<M>(p, w, key - (key - w.key0) % 32, 32))) continue;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const f32x4 x = FULL || c * 64 + qi * 4 < p.D ? *reinterpret_cast<const f32x4*>(vbase + at + c * 64 + qi * 4) : zero;
@@ -175,7 +198,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              if (key < __shfl(sees[mt], 4 * g + r)) o[mt][c][j][r] += attn_taken(x[j]);
+              if (reaches(key, mt, r)) o[mt][c][j][r] += attn_taken(x[j]);
       }
     }
   }
@@ -202,24 +225,29 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
   if (p.slots) attn_finish<float>(p, w, 16 * MT, reinterpret_cast<float*>(smem));
 }
 
-template <int DP>
+template <int M, int DP>
 hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
   const dim3 grid((unsigned)((long)p.B * p.Hkv * p.row_tiles * p.splits));
   const size_t lds = (size_t)waves * 16 * ((DP + 4) * 4 + 8);
   const auto go = [&](auto kernel) { kernel<<<grid, waves * 64, lds, st>>>(p); };
   if (mt == 1)
-    go(p.D == DP ? paged_attn_f32_kernel<DP, 1, true> : paged_attn_f32_kernel<DP, 1, false>);
+    go(p.D == DP ? paged_attn_f32_kernel<M, DP, 1, true> : paged_attn_f32_kernel<M, DP, 1, false>);
   else if constexpr (DP <= 128)
-    go(p.D == DP ? paged_attn_f32_kernel<DP, 2, true> : paged_attn_f32_kernel<DP, 2, false>);
+    go(p.D == DP ? paged_attn_f32_kernel<M, DP, 2, true> : paged_attn_f32_kernel<M, DP, 2, false>);
   return hipGetLastError();
+}
+
+template <int M>
+hipError_t launch_mask(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
+  if (p.D <= 64) return launch_dp<M, 64>(p, mt, waves, st);
+  if (p.D <= 128) return launch_dp<M, 128>(p, mt, waves, st);
+  return launch_dp<M, 256>(p, mt, waves, st);
 }
 
 }  // namespace
 
 hipError_t launch_paged_attn_f32(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
-  if (p.D <= 64) return launch_dp<64>(p, mt, waves, st);
-  if (p.D <= 128) return launch_dp<128>(p, mt, waves, st);
-  return launch_dp<256>(p, mt, waves, st);
+  return p.mask == kCausal ? launch_mask<kCausal>(p, mt, waves, st) : p.mask == kWindow ? launch_mask<kWindow>(p, mt, waves, st) : launch_mask<kTree>(p, mt, waves, st);
 }
 
 }  // namespace tsd

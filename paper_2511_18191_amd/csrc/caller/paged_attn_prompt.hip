@@ -29,16 +29,24 @@ __device__ __forceinline__ int turn(int r) {
   return DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
 }
 
-template <int DP, int WAVES, bool FULL, bool LSE>  // FULL: head_dim is DP; LSE: the logarithms are asked for
+template <int M, int DP, int WAVES, bool FULL, bool LSE>  // M: AttnMask; FULL: head_dim is DP; LSE: the logarithms are asked for
 __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int kWaveRows = 32, KK = DP / 16, DB = DP / 32, CPR = DP / 8, THREADS = WAVES * 64, NL = kTile * CPR / THREADS;
   AttnWork w = attn_place(p, WAVES * kWaveRows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r32 = lane & 31, h = lane >> 5;
   const int* table = p.cache.table + (long)w.b * p.cache.table_stride;
-  int entry = paged_entry(p.cache, table, w.key0 + lane), next_entry = paged_entry(p.cache, table, w.key0 + kTile + lane);
-  attn_lengths(p, w, WAVES * kWaveRows);
+  int entry, next_entry;
+  if constexpr (M == kCausal) {  // (the table's entries are on their way before the lengths are there)
+    entry = paged_entry(p.cache, table, w.key0 + lane);
+    next_entry = paged_entry(p.cache, table, w.key0 + kTile + lane);
+  }
+  attn_lengths<M>(p, w, WAVES * kWaveRows);
   if (w.idle) return;
+  if constexpr (M != kCausal) {
+    entry = attn_entry<M>(p, w, table, w.key0 + lane);
+    next_entry = attn_entry<M>(p, w, table, w.key0 + kTile + lane);
+  }
   const bf16* kbase = reinterpret_cast<const bf16*>(p.cache.k) + w.hk * p.cache.head_stride;
   const bf16* vbase = reinterpret_cast<const bf16*>(p.cache.v) + w.hk * p.cache.head_stride;
   bf16* lds = reinterpret_cast<bf16*>(smem);  // [2][K, V][kTile][DP]
@@ -46,7 +54,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
   const float scale2 = fmaxf(fabsf(p.scale2), 1.2e-38f);
 
   const int row0 = w.row0 + wave * kWaveRows;
-  const int row = row0 + r32, sees = attn_sees(p, w, row);
+  const int row = row0 + r32;
+  AttnSight sees = attn_sight<M>(p, w, row);
+  uint64_t line[kTreeNodes / 64] = {};
+  if constexpr (M == kTree) {
+    short* parents = reinterpret_cast<short*>(smem);
+    attn_parents(p, w, parents);
+    sees = {0, 0, line};
+    if (row < w.rows) sees = attn_node_sight(p, w, attn_line(p, w, parents, row / p.G, line), line);
+    __syncthreads();  // (the parents' place is the first tile's)
+  }
   bf16x8 qf[KK];
   {
     const int r = min(row, w.rows - 1), t = r / p.G, hq = w.hk * p.G + r - t * p.G;
@@ -59,8 +76,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
     }
   }
   // keys that the wavefront's first and last rows see (a wavefront without rows only loads)
-  const int see_first = row0 + kWaveRows <= w.rows ? attn_sees(p, w, row0) : 0;
-  const int see_last = row0 < w.rows ? attn_sees(p, w, min(row0 + kWaveRows, w.rows) - 1) : 0;
+  int see_first = row0 + kWaveRows <= w.rows ? attn_sees(p, w, row0) : 0;
+  int see_last = row0 < w.rows ? attn_sees(p, w, min(row0 + kWaveRows, w.rows) - 1) : 0;
+  int low_first = 0, low_last = 0;  // where their windows begin
+  if constexpr (M != kCausal) {
+    see_first = row0 + kWaveRows > w.rows ? 0 : M == kTree ? w.held : see_first - w.gap;
+    if (row0 < w.rows) see_last -= w.gap;
+    low_first = M == kTree ? w.first : see_first - p.window;
+    low_last = M == kTree ? w.low_last : see_last - p.window;
+  }
 
   f32x16 o[DB];
   float m_run = -INFINITY, l_run = 0.f, l_true = 0.f;  // (l_true: of the unrounded weights)
@@ -90,19 +114,19 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
       vr[i] = in ? *reinterpret_cast<const bf16x8*>(vbase + o_r + d) : zero;
     }
   };
-  long off = attn_key_row(p, w, entry, w.key0 + lane);
+  long off = attn_key_row<M>(p, w, entry, w.key0 + lane);
   entry = next_entry;
   unsigned long long valid = __ballot(off >= 0), next_valid = 0;
   if (w.key0 < w.key1) load(off, valid);
-  off = attn_key_row(p, w, entry, w.key0 + kTile + lane);
-  entry = paged_entry(p.cache, table, w.key0 + 2 * kTile + lane);
+  off = attn_key_row<M>(p, w, entry, w.key0 + kTile + lane);
+  entry = attn_entry<M>(p, w, table, w.key0 + 2 * kTile + lane);
   int parity = 0;
   bool odd = false;
   for (int sb = w.key0; sb < w.key1; sb += kTile, valid = next_valid, parity ^= 1) {
     bf16* kt = lds + parity * 2 * kTile * DP;
     bf16* vt = kt + kTile * DP;
     next_valid = __ballot(off >= 0);
-    const bool mixed = sb + kTile > w.see_first && w.see_first < w.see_last;  // (the same in every wavefront; see attn_take_out)
+    const bool mixed = attn_mixed<M>(p, w, sb, kTile);  // (the same in every wavefront; see attn_take_out)
     if (mixed) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) odd |= attn_take_out(vr[i]);
@@ -117,11 +141,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
     __syncthreads();
     // (the entries of the tile after the next are read before loads are issued that nothing waits for yet: counted waits do not
     // survive the branches between)
-    const long later = attn_key_row(p, w, entry, sb + 2 * kTile + lane);
-    entry = paged_entry(p.cache, table, sb + 3 * kTile + lane);
+    const long later = attn_key_row<M>(p, w, entry, sb + 2 * kTile + lane);
+    entry = attn_entry<M>(p, w, table, sb + 3 * kTile + lane);
     if (sb + kTile < w.key1) load(off, next_valid);
     off = later;
-    if (sb >= see_last) continue;
+    if (sb >= see_last || (M == kWindow && sb + kTile <= low_first && sb >= p.sinks)) continue;
 
     f32x16 sc[2];  // of 32 keys each
 #pragma unroll
@@ -136,15 +160,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    const bool whole = valid == ~0ull && sb + kTile <= see_first;
+    const bool whole = valid == ~0ull && sb + kTile <= see_first && (M == kCausal || sb >= low_last || sb + kTile <= p.sinks);
     if (!whole) {
-      const int left = sees - sb - 4 * h;  // (the lane's keys are 4 h further on than these)
+      const int left = sees.sees - sb - 4 * h;  // (the lane's keys are 4 h further on than these)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const unsigned there = (unsigned)(valid >> (4 * h) >> (32 * s));
+        unsigned there = (unsigned)(valid >> (4 * h) >> (32 * s));
+        if constexpr (M != kCausal) there = ((unsigned)(valid >> (32 * s)) & attn_seen<M>(p, w, sees, sb + 32 * s)) >> (4 * h);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (!(there >> (8 * (i >> 2) + (i & 3)) & 1) || s * 32 + 8 * (i >> 2) + (i & 3) >= left) sc[s][i] = -INFINITY;
+          if (!(there >> (8 * (i >> 2) + (i & 3)) & 1) || (M == kCausal && s * 32 + 8 * (i >> 2) + (i & 3) >= left)) sc[s][i] = -INFINITY;
       }
     }
     // (maxima are those of the products; a negative factor has gone into the queries, and one of 0 is too small to tell scores apart)
@@ -201,9 +226,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
     }
   }
   if (__syncthreads_or(odd)) {
-    for (int key = attn_mixed_from(w, kTile); key < w.key1; ++key) {
-      const long at = attn_key_row(p, w, paged_entry(p.cache, table, key), key);
-      if (at < 0) continue;
+    for (int key = attn_mixed_from<M>(w, kTile); key < w.key1; ++key) {
+      const long at = attn_key_row<M>(p, w, attn_entry<M>(p, w, table, key), key);
+      if (at < 0 || (M != kCausal && !attn_mixed<M>(p, w, key - (key - w.key0) % kTile, kTile))) continue;
+      const bool reached = M == kCausal ? key < sees.sees : bool(attn_seen<M>(p, w, sees, key) & 1);
 #pragma unroll
       for (int i = 0; i < DB * 4; ++i) {
         const int d = 8 * i + 4 * h;
@@ -211,7 +237,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
         if (FULL || d < p.D) v = *reinterpret_cast<const bf16x4*>(vbase + at + d);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (key < sees) o[i >> 2][(i & 3) * 4 + j] += attn_taken((float)v[j]);
+          if (reached) o[i >> 2][(i & 3) * 4 + j] += attn_taken((float)v[j]);
       }
     }
   }
@@ -230,21 +256,23 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
   }
 }
 
-template <int DP>
+template <int M, int DP>
 hipError_t launch_dp(const PagedAttnP& p, hipStream_t st) {
   const dim3 grid((unsigned)((long)p.B * p.Hkv * p.row_tiles * p.splits));
   const auto go = [&](auto kernel) { kernel<<<grid, kPromptWaves * 64, 4 * kTile * DP * 2, st>>>(p); };
   if (p.lse)
-    go(p.D == DP ? paged_attn_prompt_kernel<DP, kPromptWaves, true, true> : paged_attn_prompt_kernel<DP, kPromptWaves, false, true>);
+    go(p.D == DP ? paged_attn_prompt_kernel<M, DP, kPromptWaves, true, true> : paged_attn_prompt_kernel<M, DP, kPromptWaves, false, true>);
   else
-    go(p.D == DP ? paged_attn_prompt_kernel<DP, kPromptWaves, true, false> : paged_attn_prompt_kernel<DP, kPromptWaves, false, false>);
+    go(p.D == DP ? paged_attn_prompt_kernel<M, DP, kPromptWaves, true, false> : paged_attn_prompt_kernel<M, DP, kPromptWaves, false, false>);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_paged_attn_prompt(const PagedAttnP& p, hipStream_t st) {
-  return p.D <= 64 ? launch_dp<64>(p, st) : launch_dp<128>(p, st);
+  if (p.mask == kCausal) return p.D <= 64 ? launch_dp<kCausal, 64>(p, st) : launch_dp<kCausal, 128>(p, st);
+  if (p.mask == kWindow) return p.D <= 64 ? launch_dp<kWindow, 64>(p, st) : launch_dp<kWindow, 128>(p, st);
+  return p.D <= 64 ? launch_dp<kTree, 64>(p, st) : launch_dp<kTree, 128>(p, st);
 }
 
 }  // namespace tsd

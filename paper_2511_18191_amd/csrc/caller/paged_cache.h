@@ -40,6 +40,8 @@ __device__ __forceinline__ long paged_row(const PagedView& c, int entry, int slo
 }
 #endif
 
+constexpr int kTreeNodes = 256;  // most nodes of a tree of drafts
+
 // A launch has fewer than 2^32 lanes.
 constexpr int64_t max_workgroups(int lanes) { return 0xFFFFFFFFll / lanes; }
 

@@ -145,6 +145,7 @@ struct Wrong : std::invalid_argument {  // becomes a ValueError
 struct WrongType : std::invalid_argument {  // becomes a TypeError
   using std::invalid_argument::invalid_argument;
 };
+struct Raised {};  // Python's own error stands
 // (the message is put together only where the check fails: some twenty of them took 1 us of a call)
 #define NEED(ok, what)                       \
   do {                                       \
@@ -242,6 +243,7 @@ PyObject* guarded(const F& body) {
     PyErr_SetString(PyExc_TypeError, e.what());
   } catch (const Wrong& e) {
     PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (const Raised&) {
   } catch (const std::exception&) {
     torch::translate_exception_to_python(std::current_exception());
   }
@@ -305,10 +307,21 @@ PyObject* rope_append_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// The new tokens of an attention call.
+struct Attended {
+  tsd_paged_cache cache;
+  int32_t b, t, h, max_len;
+  tsd_rows q, out;
+  float* lse;
+  const int32_t *lens, *n_new;
+  float scale;
+};
+
 // q, k_pool, v_pool, page_table, lens, max_len or 0, scale or NaN (head_dim ^ -1/2), n_new, out, want_lse -> (status, out, lse)
-PyObject* paged_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
+// More: what the call takes besides, given the checked tensors: it may check its own.  bytes_of and go: the library's two entries.
+template <typename More, typename Bytes, typename Go>
+PyObject* attend(PyObject* const* args, const More& more, const Bytes& bytes_of, const Go& go) {
   return guarded([&]() -> PyObject* {
-    if (n != 10 || !attn_fn) throw WrongType("paged_attn_static takes ten arguments, after bind_round()");
     const at::Tensor &q = the(args[0], "q"), &k_pool = the(args[1], "k_pool"), &v_pool = the(args[2], "v_pool"), &table = the(args[3], "page_table"),
                      &lens = the(args[4], "lens");
     const long long asked = PyLong_AsLongLong(args[5]);
@@ -332,22 +345,25 @@ PyObject* paged_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int32_t b = whole(B, "B"), t = whole(T, "T"), h = whole(H, "heads"),
                   max_len = whole(asked ? asked : (int64_t)cache.pages_per_seq * cache.page_tokens, "max_len");
     if (std::isnan(scale)) scale = 1.0 / std::sqrt((double)cache.head_dim);
+    more(q, B, T);
     const c10::DeviceGuard guard(q.device());
     size_t bytes = 0;
-    int rc = attn_bytes_fn(&cache, b, t, h, max_len, &bytes);
+    Attended a = {cache, b, t, h, max_len, rq, rq, nullptr, static_cast<const int32_t*>(lens.data_ptr()),
+                  n_new ? static_cast<const int32_t*>(n_new->data_ptr()) : nullptr, (float)scale};
+    int rc = bytes_of(a, &bytes);
     at::Tensor out = to ? *to : at::empty({B, T, H, cache.head_dim}, q.options()), lse, work;
     if (to) {
       like(out, q, "out");
       apart(out, "out");
     }
-    const tsd_rows ro = rows_of(out, q.sizes(), "out");
+    a.out = rows_of(out, q.sizes(), "out");
     if (want_lse) lse = at::empty({B, T, H}, q.options().dtype(at::kFloat));
     if (rc == TSD_OK) {
       if (bytes) work = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
       void* stream = c10::hip::getCurrentHIPStream(q.device().index()).stream();
+      a.lse = want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr;
       Py_BEGIN_ALLOW_THREADS
-      rc = attn_fn(&cache, b, t, h, &rq, &ro, want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, static_cast<const int32_t*>(lens.data_ptr()),
-                   n_new ? static_cast<const int32_t*>(n_new->data_ptr()) : nullptr, max_len, (float)scale, bytes ? work.data_ptr() : nullptr, bytes, stream);
+      rc = go(a, bytes ? work.data_ptr() : nullptr, bytes, stream);
       Py_END_ALLOW_THREADS
       if (rc == TSD_OK && to) written(out);
     }
@@ -355,6 +371,19 @@ PyObject* paged_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (!want_lse) Py_INCREF(Py_None);
     return Py_BuildValue("iNN", rc, THPVariable_Wrap(out), l);
   });
+}
+
+PyObject* paged_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 10 || !attn_fn) {
+    PyErr_SetString(PyExc_TypeError, "paged_attn_static takes ten arguments, after bind_round()");
+    return nullptr;
+  }
+  return attend(
+      args, [](const at::Tensor&, int64_t, int64_t) {},
+      [](const Attended& a, size_t* bytes) { return attn_bytes_fn(&a.cache, a.b, a.t, a.h, a.max_len, bytes); },
+      [](const Attended& a, void* work, size_t bytes, void* stream) {
+        return attn_fn(&a.cache, a.b, a.t, a.h, &a.q, &a.out, a.lse, a.lens, a.n_new, a.max_len, a.scale, work, bytes, stream);
+      });
 }
 
 // draft, q or None, p, uniforms, n_draft -> (status, n_acc, tokens)
@@ -399,6 +428,233 @@ PyObject* verify_tokens_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// ---- rounds of drafted trees, windowed caches, scores ----------------------------------------------------------------------------
+decltype(&tsd_window_attn_workspace) window_bytes_fn = nullptr;
+decltype(&tsd_window_attn_static) window_fn = nullptr;
+decltype(&tsd_tree_attn_workspace) tree_bytes_fn = nullptr;
+decltype(&tsd_tree_attn_static) tree_fn = nullptr;
+decltype(&tsd_token_logprobs_workspace) scores_bytes_fn = nullptr;
+decltype(&tsd_token_logprobs_static) scores_fn = nullptr;
+decltype(&tsd_verify_tree_workspace) walk_bytes_fn = nullptr;
+decltype(&tsd_verify_tree_static) walk_fn = nullptr;
+decltype(&tsd_keep_path_static) keep_fn = nullptr;
+
+// (the nine functions' addresses, in the order above)
+PyObject* bind_trees(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  void* p[9];
+  if (n != 9) {
+    PyErr_SetString(PyExc_TypeError, "bind_trees takes nine addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 9; ++i) {
+    p[i] = PyLong_AsVoidPtr(args[i]);
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind_trees: an address is 0");
+      return nullptr;
+    }
+  }
+  window_bytes_fn = reinterpret_cast<decltype(window_bytes_fn)>(p[0]);
+  window_fn = reinterpret_cast<decltype(window_fn)>(p[1]);
+  tree_bytes_fn = reinterpret_cast<decltype(tree_bytes_fn)>(p[2]);
+  tree_fn = reinterpret_cast<decltype(tree_fn)>(p[3]);
+  scores_bytes_fn = reinterpret_cast<decltype(scores_bytes_fn)>(p[4]);
+  scores_fn = reinterpret_cast<decltype(scores_fn)>(p[5]);
+  walk_bytes_fn = reinterpret_cast<decltype(walk_bytes_fn)>(p[6]);
+  walk_fn = reinterpret_cast<decltype(walk_fn)>(p[7]);
+  keep_fn = reinterpret_cast<decltype(keep_fn)>(p[8]);
+  Py_RETURN_NONE;
+}
+
+int32_t number(PyObject* o, const char* name) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Raised();
+  NEED(v >= INT32_MIN && v <= INT32_MAX, std::string(name) + " is out of range");
+  return (int32_t)v;
+}
+
+// Parents of the nodes of trees, [B, N] or [N]: their rows' distance.
+int32_t parents_of(const at::Tensor& parents, const at::Tensor& first, int64_t B, int64_t N) {
+  if (parents.dim() == 1)
+    plain(parents, first, at::kInt, {N}, "parents");
+  else
+    plain(parents, first, at::kInt, {B, N}, "parents");
+  return parents.dim() == 1 ? 0 : (int32_t)N;
+}
+
+// ..., window, sinks
+PyObject* window_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 12 || !window_fn) {
+    PyErr_SetString(PyExc_TypeError, "window_attn_static takes twelve arguments, after bind_trees()");
+    return nullptr;
+  }
+  int32_t window = 0, sinks = 0;
+  return attend(
+      args,
+      [&](const at::Tensor&, int64_t, int64_t) {
+        window = number(args[10], "window");
+        sinks = number(args[11], "sinks");
+      },
+      [&](const Attended& a, size_t* bytes) { return window_bytes_fn(&a.cache, a.b, a.t, a.h, a.max_len, window, sinks, bytes); },
+      [&](const Attended& a, void* work, size_t bytes, void* stream) {
+        return window_fn(&a.cache, a.b, a.t, a.h, &a.q, &a.out, a.lse, a.lens, a.n_new, a.max_len, window, sinks, a.scale, work, bytes, stream);
+      });
+}
+
+// ..., window or 0, sinks, parents
+PyObject* tree_attn_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 13 || !tree_fn) {
+    PyErr_SetString(PyExc_TypeError, "tree_attn_static takes thirteen arguments, after bind_trees()");
+    return nullptr;
+  }
+  int32_t window = 0, sinks = 0, stride = 0;
+  const int32_t* parents = nullptr;
+  return attend(
+      args,
+      [&](const at::Tensor& q, int64_t B, int64_t T) {
+        window = number(args[10], "window");
+        sinks = number(args[11], "sinks");
+        const at::Tensor& t = the(args[12], "parents");
+        stride = parents_of(t, q, B, T);
+        parents = static_cast<const int32_t*>(t.data_ptr());
+      },
+      [&](const Attended& a, size_t* bytes) { return tree_bytes_fn(&a.cache, a.b, a.t, a.h, a.max_len, window, sinks, bytes); },
+      [&](const Attended& a, void* work, size_t bytes, void* stream) {
+        return tree_fn(&a.cache, a.b, a.t, a.h, &a.q, &a.out, a.lse, a.lens, a.n_new, parents, stride, a.max_len, window, sinks, a.scale, work, bytes, stream);
+      });
+}
+
+PyObject* or_none(const at::Tensor& t) {
+  if (t.defined()) return THPVariable_Wrap(t);
+  Py_RETURN_NONE;
+}
+
+// logits, tokens or None, top, temperature, n_new -> (status, logprobs, entropy, top_ids, top_logprobs)
+PyObject* token_logprobs_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 5 || !scores_fn) throw WrongType("token_logprobs_static takes five arguments, after bind_trees()");
+    const at::Tensor& logits = the(args[0], "logits");
+    const at::Tensor *tokens = maybe(args[1], "tokens"), *n_new = maybe(args[4], "n_new");
+    const long long asked = PyLong_AsLongLong(args[2]);
+    const double temperature = PyFloat_AsDouble(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    if (c10::GradMode::is_enabled()) no_gradient(logits, "logits");
+    on_gpu(logits, "logits");
+    const int dtype = dtype_of(logits, "logits");
+    NEED(logits.dim() == 3 && (logits.size(2) < 2 || logits.stride(2) == 1), "logits must be [B, T, V], rows dense");
+    const int64_t B = logits.size(0), T = logits.size(1);
+    if (tokens) {
+      NEED(tokens->scalar_type() == at::kInt || tokens->scalar_type() == at::kLong, "tokens must be int32 or int64");
+      plain(*tokens, logits, tokens->scalar_type(), {B, T}, "tokens");
+    }
+    if (n_new) plain(*n_new, logits, at::kInt, {B}, "n_new");
+    const int32_t b = whole(B, "B"), t = whole(T, "T"), v = whole(logits.size(2), "V"), top = whole(asked, "top");
+    const c10::DeviceGuard guard(logits.device());
+    size_t bytes = 0;
+    int rc = scores_bytes_fn(b, t, v, top, &bytes);
+    at::Tensor logprobs, entropy, ids, alternatives, work;
+    if (rc == TSD_OK) {
+      const auto f32 = logits.options().dtype(at::kFloat);
+      if (tokens) logprobs = at::empty({B, T}, f32);
+      entropy = at::empty({B, T}, f32);
+      if (top) {
+        ids = at::empty({B, T, top}, f32.dtype(at::kInt));
+        alternatives = at::empty({B, T, top}, f32);
+      }
+      if (bytes) work = at::empty({(int64_t)bytes}, f32.dtype(at::kByte));
+      const auto at_of = [](const at::Tensor& x) { return x.defined() ? x.data_ptr() : nullptr; };
+      void* stream = c10::hip::getCurrentHIPStream(logits.device().index()).stream();
+      Py_BEGIN_ALLOW_THREADS
+      rc = scores_fn(logits.data_ptr(), dtype, tokens ? (int32_t)tokens->element_size() : 0, b, t, v, logits.stride(0), logits.stride(1),
+                     tokens ? tokens->data_ptr() : nullptr, n_new ? static_cast<const int32_t*>(n_new->data_ptr()) : nullptr, (float)temperature, top,
+                     static_cast<float*>(at_of(logprobs)), static_cast<float*>(at_of(entropy)), static_cast<int32_t*>(at_of(ids)),
+                     static_cast<float*>(at_of(alternatives)), at_of(work), bytes, stream);
+      Py_END_ALLOW_THREADS
+    }
+    return Py_BuildValue("iNNNN", rc, or_none(logprobs), or_none(entropy), or_none(ids), or_none(alternatives));
+  });
+}
+
+// tokens, parents, p or None, uniforms or None, choices or None, n_new -> (status, n_acc, tokens, path)
+PyObject* verify_tree_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 6 || !walk_fn) throw WrongType("verify_tree_static takes six arguments, after bind_trees()");
+    const at::Tensor &tokens = the(args[0], "tokens"), &parents = the(args[1], "parents");
+    const at::Tensor *p = maybe(args[2], "p"), *uniforms = maybe(args[3], "uniforms"), *choices = maybe(args[4], "choices"), *n_new = maybe(args[5], "n_new");
+    on_gpu(tokens, "tokens");
+    NEED(tokens.scalar_type() == at::kInt || tokens.scalar_type() == at::kLong, "tokens must be int32 or int64");
+    NEED(tokens.dim() == 2, "tokens must be [B, N]");
+    const int64_t B = tokens.size(0), N = tokens.size(1);
+    plain(tokens, tokens, tokens.scalar_type(), {B, N}, "tokens");
+    const int32_t stride = parents_of(parents, tokens, B, N);
+    NEED(!p == !uniforms && !p == !!choices, "needs either p and uniforms, or choices");
+    int dtype = TSD_F32;
+    if (p) {
+      NEED(p->device() == tokens.device(), "p is on " + p->device().str() + ", not on " + tokens.device().str());
+      dtype = dtype_of(*p, "p");
+      NEED(p->dim() == 3 && p->size(0) == B && p->size(1) == N && (p->size(2) < 2 || p->stride(2) == 1), "p must be [B, N, V], rows dense");
+      plain(*uniforms, tokens, at::kFloat, {B, N}, "uniforms");
+    } else {
+      plain(*choices, tokens, tokens.scalar_type(), {B, N}, "choices");
+    }
+    if (n_new) plain(*n_new, tokens, at::kInt, {B}, "n_new");
+    const int32_t b = whole(B, "B"), nn = whole(N, "N"), v = p ? whole(p->size(2), "V") : 1;
+    const c10::DeviceGuard guard(tokens.device());
+    size_t bytes = 0;
+    int rc = walk_bytes_fn(b, nn, v, dtype, &bytes);
+    at::Tensor n_acc, out, path, work;
+    if (rc == TSD_OK) {
+      n_acc = at::empty({B}, tokens.options().dtype(at::kInt));
+      out = at::empty({B, N}, tokens.options());
+      path = at::empty({B, N}, tokens.options().dtype(at::kInt));
+      if (p && bytes) work = at::empty({(int64_t)bytes}, tokens.options().dtype(at::kByte));
+      void* stream = c10::hip::getCurrentHIPStream(tokens.device().index()).stream();
+      Py_BEGIN_ALLOW_THREADS
+      rc = walk_fn(tokens.data_ptr(), static_cast<const int32_t*>(parents.data_ptr()), stride, p ? p->data_ptr() : nullptr, dtype,
+                   (int32_t)tokens.element_size(), b, nn, v, p ? p->stride(0) : 0, p ? p->stride(1) : 0,
+                   uniforms ? static_cast<const float*>(uniforms->data_ptr()) : nullptr, choices ? choices->data_ptr() : nullptr,
+                   n_new ? static_cast<const int32_t*>(n_new->data_ptr()) : nullptr, static_cast<int32_t*>(n_acc.data_ptr()), out.data_ptr(),
+                   static_cast<int32_t*>(path.data_ptr()), work.defined() ? work.data_ptr() : nullptr, work.defined() ? bytes : 0, stream);
+      Py_END_ALLOW_THREADS
+    }
+    return Py_BuildValue("iNNN", rc, or_none(n_acc), or_none(out), or_none(path));
+  });
+}
+
+// k_pool, v_pool, page_table, held, path -> status
+PyObject* keep_path_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 5 || !keep_fn) throw WrongType("keep_path_static takes five arguments, after bind_trees()");
+    const at::Tensor &k = the(args[0], "k_pool"), &v = the(args[1], "v_pool"), &table = the(args[2], "page_table"), &held = the(args[3], "held"),
+                     &path = the(args[4], "path");
+    if (c10::GradMode::is_enabled()) {
+      no_gradient(k, "k_pool");
+      no_gradient(v, "v_pool");
+    }
+    NEED(path.dim() == 2, "path must be [B, N]");
+    const int64_t B = path.size(0), N = path.size(1);
+    const bool layers = k.dim() == 5;
+    NEED(!layers || (v.sizes() == k.sizes() && v.strides() == k.strides()), "k_pool and v_pool must have the same shape and strides");
+    NEED(!layers || k.size(0) > 0, "k_pool: needs a layer");
+    const tsd_paged_cache cache = layers ? cache_of(k.select(0, 0), v.select(0, 0), table, B) : cache_of(k, v, table, B);
+    apart(k, "k_pool");
+    apart(v, "v_pool");
+    plain(held, k, at::kInt, {B}, "held");
+    plain(path, k, at::kInt, {B, N}, "path");
+    const int32_t b = whole(B, "B"), nn = whole(N, "N"), l = layers ? whole(k.size(0), "k_pool") : 1;
+    const c10::DeviceGuard guard(k.device());
+    void* stream = c10::hip::getCurrentHIPStream(k.device().index()).stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = keep_fn(&cache, l, l > 1 ? k.stride(0) : 0, b, nn, static_cast<const int32_t*>(held.data_ptr()), static_cast<const int32_t*>(path.data_ptr()), stream);
+    Py_END_ALLOW_THREADS
+    if (rc == TSD_OK) {
+      written(k);
+      written(v);
+    }
+    return PyLong_FromLong(rc);
+  });
+}
+
 template <typename F>
 PyCFunction fast(F* f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f));
@@ -411,6 +667,12 @@ PyMethodDef methods[] = {{"bind", bind, METH_O, "the address of tsd_accept_commi
                          {"rope_append_static", fast(rope_append_static), METH_FASTCALL, "see binding.rope_append_static"},
                          {"paged_attn_static", fast(paged_attn_static), METH_FASTCALL, "see binding.paged_attn_static"},
                          {"verify_tokens_static", fast(verify_tokens_static), METH_FASTCALL, "see binding.verify_tokens_static"},
+                         {"bind_trees", fast(bind_trees), METH_FASTCALL, "the addresses of the calls of a round of trees"},
+                         {"window_attn_static", fast(window_attn_static), METH_FASTCALL, "see binding.window_attn_static"},
+                         {"tree_attn_static", fast(tree_attn_static), METH_FASTCALL, "see binding.tree_attn_static"},
+                         {"token_logprobs_static", fast(token_logprobs_static), METH_FASTCALL, "see binding.token_logprobs_static"},
+                         {"verify_tree_static", fast(verify_tree_static), METH_FASTCALL, "see binding.verify_tree_static"},
+                         {"keep_path_static", fast(keep_path_static), METH_FASTCALL, "see binding.keep_path_static"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
