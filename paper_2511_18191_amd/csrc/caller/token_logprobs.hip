@@ -5,12 +5,16 @@
 // the maximum itself are taken before the factor: logits may be as large as their type's largest.)
 //
 // One pass over the row.  For the alternatives each lane's maxima of kCell elements stay in LDS.  A bound that at least `top` elements reach is had
-// without a sort: of each wavefront's lanes the (top / 4)-th largest maximum, and of these the least.  Only cells that reach it are read again (some top of
-// them, out of the last cache), and what reaches it there, a few more than top, is ranked by counting.  Where more elements reach the bound than LDS has
-// room for (masks of one finite value, say), those above it and then as many at it as are needed, in the order of the row; where that does
+// by counting: of the maxima of all lanes, in fours, it is the top-th.  Only cells that reach it are read again (some
+// top of them, out of the last cache), and what reaches it there, a few more than top, is ranked by counting too.  Where more elements reach the bound than
+// LDS has room for (masks of one finite value, say), those above it and then as many at it as are needed, in the order of the row; where that does
 // not fit either, one after the other.
 //
-// A row takes one workgroup, or, where rows are few, several; the one that comes last joins their sums and lists (last_arriver.h).
+// A row takes one workgroup, or, where long rows are few, several; the one that comes last joins their sums and lists (last_arriver.h).
+//
+// Many rows are memory bound: 1024 rows of 131072 bf16 logits 52.6 us without alternatives, 5.1 TB/s (what a copy reaches), 59 us with twenty, whose bounds
+// and second looks are not hidden in full.  A row of 32000 fp32: 6.6 us, and 9.3 with five alternatives; the launch, two trips to memory, and for
+// alternatives a third behind four barriers.  (1024 lanes a workgroup: 7.9 and 14; bounds from every wavefront's sorted maxima: 10.3.)
 #include <algorithm>
 #include <cmath>
 
@@ -20,10 +24,9 @@
 namespace tsd {
 namespace {
 
-constexpr int kLanes = 256;
+constexpr int kLanes = 256;                  // of a workgroup
 constexpr int kCell = 64;                    // elements of a lane whose maximum is kept
-constexpr int kBlock = kLanes * kCell;       // elements that a workgroup takes at a time
-constexpr int kMostBlocks = 16;              // of a workgroup: its maxima are in LDS
+constexpr int kMostPart = 262144;            // elements of a workgroup: its maxima are in LDS
 constexpr int kMostTop = 32;
 constexpr int kMostGroups = 32;              // workgroups of a row
 constexpr int kMostCells = 512, kMostFound = 1024;  // cells and elements that reach the bound, in LDS
@@ -117,10 +120,19 @@ __device__ __forceinline__ void load_cells(const Part<T>& q, int i, int c0, floa
     for (int j = 0; j < U * E; ++j) x[j] = element<T>(y[j / E], j % E);
   } else {
 #pragma unroll
-    for (int j = 0; j < U * E; ++j) {
-      const int at = q.start(i, c0 + j / E, threadIdx.x) + j % E;
-      x[j] = -INFINITY;
-      if (at < q.n) x[j] = (float)q.p[at];
+    for (int u = 0; u < U; ++u) {
+      const int at = q.start(i, c0 + u, threadIdx.x);
+      if (q.start(i, c0 + u + 1, 0) <= q.n) {
+        const Words y = load_pack(q.p + at);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[u * E + e] = element<T>(y, e);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          x[u * E + e] = -INFINITY;
+          if (at + e < q.n) x[u * E + e] = (float)q.p[at + e];
+        }
+      }
     }
   }
 }
@@ -128,30 +140,28 @@ __device__ __forceinline__ void load_cells(const Part<T>& q, int i, int c0, floa
 // The `top` largest of n keys in LDS, ranked: put(rank, key).
 template <typename Put>
 __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int top, Put put) {
-  for (int i = threadIdx.x; i < n; i += kLanes) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const uint64_t own = keys[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) rank += keys[j] > own;
     if (rank < top) put(rank, own);
   }
 }
 
-// The workgroup's: what finding the alternatives needs.
+// What finding the alternatives needs in LDS.
 struct Candidates {
   uint64_t keys[kMostFound];
-  float lane_max[kLanes];
-  float bound[kLanes / 64];
   int cells[kMostCells];
   int n_cells, n_found, ties[kLanes / 64];
   uint64_t best[kLanes / 64];
+  float maxima[kLanes / 4];
+  float bound;
 };
 
-// The elements of cells that reach `bound` (above: exceed it) into LDS; whether they fit.
+// The elements of cells that reach `bound` (above: exceed it) into LDS, whose counts are 0; whether they fit.
 template <typename T>
 __device__ __forceinline__ bool collect(const Part<T>& q, long base, const float* maxima, int blocks, float bound, bool above, Candidates& f) {
-  __syncthreads();
-  if (threadIdx.x == 0) f.n_cells = f.n_found = 0;
-  __syncthreads();
   const auto in = [&](float x) { return above ? x > bound : x >= bound && x > -INFINITY; };
   for (int i = threadIdx.x; i < blocks * kLanes; i += kLanes)
     if (in(maxima[i])) {
@@ -238,24 +248,35 @@ __device__ __forceinline__ void extract(const Part<T>& q, long base, int top, Ca
 // The part's elements among which its `top` largest are, as keys in LDS.
 template <typename T>
 __device__ __forceinline__ void find_top(const Part<T>& q, long base, const float* maxima, int blocks, float lane_max, int top, Candidates& f) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  f.lane_max[threadIdx.x] = lane_max;
+  static_assert(kLanes / 4 == 64);
+  lane_max = fmaxf(lane_max, __shfl_xor(lane_max, 1));
+  lane_max = fmaxf(lane_max, __shfl_xor(lane_max, 2));
+  if ((threadIdx.x & 3) == 0) f.maxima[threadIdx.x >> 2] = lane_max;
   __syncthreads();
-  // of a wavefront's maxima the largest that at least `each` reach
-  const int each = (top + kLanes / 64 - 1) / (kLanes / 64);
-  int reach = 0;
+  if (threadIdx.x < 64) {  // (the largest value that at least `top` of the 64 reach)
+    const float own = f.maxima[threadIdx.x];
+    int reach = 0;
 #pragma unroll
-  for (int j = 0; j < 64; ++j) reach += f.lane_max[wave * 64 + j] >= lane_max;
-  float b = reach >= each ? lane_max : -INFINITY;
+    for (int j = 0; j < 64; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own), j)) >= own;
+    float b = reach >= top ? own : -INFINITY;
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) b = fmaxf(b, __shfl_xor(b, o));
-  if (lane == 0) f.bound[wave] = b;
+    for (int o = 32; o >= 1; o >>= 1) b = fmaxf(b, __shfl_xor(b, o));
+    if (threadIdx.x == 0) {
+      f.bound = b;
+      f.n_cells = f.n_found = 0;
+    }
+  }
   __syncthreads();
-  const float bound = fminf(fminf(f.bound[0], f.bound[1]), fminf(f.bound[2], f.bound[3]));
+  const float bound = f.bound;
   if (collect(q, base, maxima, blocks, bound, false, f)) return;
-  if (bound > -INFINITY && collect(q, base, maxima, blocks, bound, true, f)) {
-    collect_ties(q, base, bound, top - f.n_found, f);
-    return;
+  if (bound > -INFINITY) {
+    __syncthreads();
+    if (threadIdx.x == 0) f.n_cells = f.n_found = 0;
+    __syncthreads();
+    if (collect(q, base, maxima, blocks, bound, true, f)) {
+      collect_ties(q, base, bound, top - f.n_found, f);
+      return;
+    }
   }
   extract(q, base, top, f);
 }
@@ -267,9 +288,16 @@ __device__ __forceinline__ void put_row(const ScoreP& a, long row, const Sums& z
   if (a.logprobs) a.logprobs[row] = none || !there ? (z.s != z.s ? z.s : -INFINITY) : (x - z.m) * a.inv - ln_s;
   a.entropy[row] = none ? 0.f : ln_s - z.w / z.s * 0.69314718055994531f;
 }
-__device__ __forceinline__ void put_alternative(const ScoreP& a, long row, int rank, const Sums& z, uint64_t key) {
-  a.top_ids[row * a.top + rank] = (int)index_of(key);
-  a.top_logprobs[row * a.top + rank] = (value_of(key) - z.m) * a.inv - logf(z.s);
+// The likeliest of the keys in LDS.
+__device__ __forceinline__ void put_top(const ScoreP& a, long row, const Sums& z, const Candidates& f) {
+  rank_keys(f.keys, f.n_found, a.top, [&](int rank, uint64_t key) {
+    a.top_ids[row * a.top + rank] = (int)index_of(key);
+    a.top_logprobs[row * a.top + rank] = (value_of(key) - z.m) * a.inv - logf(z.s);
+  });
+  if (threadIdx.x >= f.n_found && threadIdx.x < a.top) {
+    a.top_ids[row * a.top + threadIdx.x] = -1;
+    a.top_logprobs[row * a.top + threadIdx.x] = -INFINITY;
+  }
 }
 
 template <typename T, bool TOP>
@@ -299,7 +327,7 @@ __global__ __launch_bounds__(kLanes) void token_logprobs_kernel(const ScoreP a) 
 
   const long base = (long)group * a.per;
   const Part<T> q = {whole + base, (int)min((long)a.per, a.V - base)};
-  const int blocks = (q.n + kBlock - 1) / kBlock;
+  const int blocks = (q.n + kLanes * kCell - 1) / (kLanes * kCell);
   constexpr int U = 8, N = U * Part<T>::E;
   Sums z = kNoSums;
   for (int i = 0; i < blocks; ++i) {
@@ -331,13 +359,7 @@ __global__ __launch_bounds__(kLanes) void token_logprobs_kernel(const ScoreP a) 
 
   if (a.groups == 1) {
     if (threadIdx.x == 0) put_row(a, row, z, x_token, there);
-    if constexpr (TOP) {
-      rank_keys(found.keys, found.n_found, a.top, [&](int rank, uint64_t key) { put_alternative(a, row, rank, z, key); });
-      if (threadIdx.x >= found.n_found && threadIdx.x < a.top) {
-        a.top_ids[row * a.top + threadIdx.x] = -1;
-        a.top_logprobs[row * a.top + threadIdx.x] = -INFINITY;
-      }
-    }
+    if constexpr (TOP) put_top(a, row, z, found);
     return;
   }
   const long at = row * a.groups + group;
@@ -369,62 +391,59 @@ __global__ __launch_bounds__(kLanes) void token_logprobs_kernel(const ScoreP a) 
   }
   if (threadIdx.x == 0) put_row(a, row, z, x_token, there);
   if constexpr (TOP) {
-    // the lists' heads, 256 of all, give a bound that at least `top` keys reach; those are ranked
+    // The lists' heads, 64 in all, give a bound that at least `top` keys reach; those are ranked.
     Candidates& f = found;
     const uint64_t* lists = a.lists + row * a.groups * a.top;
     const int n = a.groups * a.top;
-    for (int i = threadIdx.x; i < n; i += kLanes) f.keys[i] = left(lists + i);
-    __syncthreads();
-    const int heads = min(a.top, kLanes / a.groups), g = threadIdx.x / heads;
-    uint64_t own = g < a.groups ? f.keys[g * a.top + threadIdx.x - g * heads] : 0;
-    int reach = 0;
-    for (int u = 0; u < a.groups; ++u)
-      for (int j = 0; j < heads; ++j) reach += f.keys[u * a.top + j] >= own;
-    if (g >= a.groups || reach < a.top) own = 0;
+    constexpr int U = kMostFound / kLanes;
+    uint64_t key[U];
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) own = max(own, (uint64_t)__shfl_xor((unsigned long long)own, o));
-    if (lane == 0) f.best[wave] = own;
-    __syncthreads();
-    for (int v = 0; v < kLanes / 64; ++v) own = max(own, f.best[v]);
-    // (keys in order: those that do not reach the bound come to nothing)
-    int count = 0;
-    for (int i = threadIdx.x; i < n; i += kLanes) {
-      const uint64_t key = f.keys[i];
-      if (!key || key < own) continue;
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += f.keys[j] > key;
-      if (rank < a.top) {
-        put_alternative(a, row, rank, z, key);
-        ++count;
-      }
-    }
+    for (int u = 0; u < U; ++u) key[u] = u * kLanes < n ? left(lists + min(u * kLanes + (int)threadIdx.x, n - 1)) : 0;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) count += __shfl_xor(count, o);
-    if (lane == 0) f.ties[wave] = count;
-    __syncthreads();
-    count = 0;
-    for (int v = 0; v < kLanes / 64; ++v) count += f.ties[v];
-    if (threadIdx.x >= count && threadIdx.x < a.top) {
-      a.top_ids[row * a.top + threadIdx.x] = -1;
-      a.top_logprobs[row * a.top + threadIdx.x] = -INFINITY;
+    for (int u = 0; u < U; ++u) {
+      if (u * kLanes + threadIdx.x >= n) key[u] = 0;
+      if (u * kLanes < n) f.keys[u * kLanes + threadIdx.x] = key[u];
     }
+    if (threadIdx.x == 0) f.n_found = 0;
+    __syncthreads();
+    if (wave == 0) {
+      const int heads = min(a.top, 64 / a.groups), g = lane / heads;
+      const uint64_t own = g < a.groups ? f.keys[g * a.top + lane - g * heads] : 0;
+      int reach = 0;
+#pragma unroll
+      for (int j = 0; j < 64; ++j)
+        reach += ((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(own >> 32), j) << 32 | (unsigned)__builtin_amdgcn_readlane((int)own, j)) >= own;
+      uint64_t b = reach < a.top ? 0 : own;
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) b = max(b, (uint64_t)__shfl_xor((unsigned long long)b, o));
+      if (lane == 0) f.best[0] = b;
+    }
+    __syncthreads();
+    const uint64_t bound = f.best[0];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (key[u] && key[u] >= bound) f.keys[atomicAdd(&f.n_found, 1)] = key[u];
+    __syncthreads();
+    put_top(a, row, z, f);
   }
   clear_slots(slots, a.groups);
 }
 
-// Workgroups of a row: some 512 in all, none with less than 1024 elements, all with as many as LDS has maxima for.
+// Workgroups of a row: one, but for long rows that are few, whose join (4 us) pays: then some 512 in all, with 8192 elements at least.  us with 1, 4, 8 and 16 a
+// row (fp32, five alternatives): 32000 x 1 row 9.3, 10.4, 11.6, 11.7, x 256 12.1, 18.0, 26.6, 42.0; 131072 x 1 17.1, 12.6, 12.0, 11.3, x 64 20.9,
+// 16.0, 16.1, 17.7, x 128 26.5, 22.3, 23.1, 27.6, x 256 29.5, 35.0, 38.9, 43.4; 262144 x 1 34.1, 15.3, 13.4, 12.0.
 struct ScorePlan {
   int groups, per;
 };
 ScorePlan score_plan(int64_t rows, int V) {
-  const int64_t least = (V + (int64_t)kMostBlocks * kBlock - 1) / (kMostBlocks * kBlock);
-  const int64_t want = std::max(least, std::min<int64_t>({kMostGroups, (V + 1023) / 1024, std::max<int64_t>(1, 512 / rows)}));
+  int64_t want = V <= 65536 || rows >= 192 ? 1 : std::min<int64_t>({16, V / 8192, 512 / rows});
+  want = std::max(want, (V + (int64_t)kMostPart - 1) / kMostPart);
   ScorePlan s;
   s.per = (int)((V + want - 1) / want + 1023) / 1024 * 1024;
   s.groups = (V + s.per - 1) / s.per;
   return s;
 }
-constexpr int kMostTokensScored = kMostBlocks * kBlock * kMostGroups;
+constexpr int kMostTokensScored = kMostPart * kMostGroups;
 
 int check_scores(int32_t B, int32_t T, int32_t V, int32_t top) {
   if (B < 1 || T < 1 || V < 1) return fail_no_handle(TSD_E_INVALID_ARG, "need B >= 1, T >= 1 and V >= 1");
@@ -493,13 +512,8 @@ extern "C" int tsd_token_logprobs_static(const void* logits_dev, int32_t dtype, 
   a.tag = s.groups > 1 ? new_tag() : 0;
   const hipStream_t st = (hipStream_t)stream;
   const unsigned grid = (unsigned)(rows * s.groups);
-  const size_t lds = top ? (size_t)((s.per + kBlock - 1) / kBlock) * kLanes * 4 : 0;
-  const auto go = [&](auto with, auto without) {
-    if (top)
-      with<<<grid, kLanes, lds, st>>>(a);
-    else
-      without<<<grid, kLanes, lds, st>>>(a);
-  };
+  const size_t lds = top ? (size_t)((s.per + kLanes * kCell - 1) / (kLanes * kCell)) * kLanes * 4 : 0;
+  const auto go = [&](auto with, auto without) { (top ? with : without)<<<grid, kLanes, lds, st>>>(a); };
   if (dtype == TSD_BF16)
     go(token_logprobs_kernel<bf16, true>, token_logprobs_kernel<bf16, false>);
   else
