@@ -386,7 +386,7 @@ int tsd_token_logprobs_static(const void* logits_dev, int32_t dtype, int32_t tok
  *   n_acc_dev int32 [B]: drafted nodes on the way; tokens out_dev [B][N] of the tokens' type: theirs, the last token drawn, -1 behind it;
  *   path_dev int32 [B][N]: node 0, the nodes on the way, -1 behind them.
  * n_new_dev int32 [B] (NULL: N each; clamped to 0..N): the nodes that are there; without any n_acc is -1, everything else too.  N <= 256, V <= 2^21
- * (TSD_E_OUT_OF_RANGE).  workspace_dev: tsd_verify_tree_workspace bytes (often 0; not looked at for choices), 8-byte aligned, as above. */
+ * (TSD_E_OUT_OF_RANGE).  workspace_dev: tsd_verify_tree_workspace bytes (often 0; not looked at for choices), 4-byte aligned, as above. */
 int tsd_verify_tree_workspace(int32_t B, int32_t N, int32_t V, int32_t dtype, size_t* bytes_host);
 int tsd_verify_tree_static(const void* tokens_dev, const int32_t* parents_dev, int32_t parents_stride, const void* p_dev, int32_t dtype,
                            int32_t token_bytes, int32_t B, int32_t N, int32_t V, int64_t p_stride_b, int64_t p_stride_n, const float* uniforms_dev,

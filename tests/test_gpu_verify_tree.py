@@ -40,7 +40,7 @@ def run(tokens, parents, p=None, u=None, choices=None, n_new=None):
 @pytest.mark.parametrize("dtype", [FP, BF])
 @pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("B,N,V", [(1, 1, 1), (1, 1, 1000), (3, 2, 2), (5, 7, 40), (4, 26, 1000), (2, 64, 1024), (3, 65, 1025), (1, 256, 300), (2, 20, 32000),
-                                   (40, 12, 5000), (1, 8, 131072), (300, 5, 257)])
+                                   (40, 12, 5000), (1, 8, 131072), (3, 9, 65537), (9, 30, 70001), (300, 5, 257)])
 def test_sizes(dtype, wide, B, N, V):
     run(*inputs(B, N, V, dtype, wide=wide))
 
@@ -63,26 +63,35 @@ def test_one_tree_for_all():
     run(tokens, parents[0].contiguous(), p, u)
 
 
-def test_ragged_and_empty():
-    tokens, parents, p, u = inputs(7, 15, 100, sharp=8.0)
+@pytest.mark.parametrize("V", [100, 66000])
+def test_ragged_and_empty(V):
+    tokens, parents, p, u = inputs(7, 15, V, sharp=8.0)
     n_new = torch.tensor([0, 1, 2, 15, 99, -4, 8], dtype=torch.int32).cuda()
     n_acc = run(tokens, parents, p, u, n_new=n_new)
     assert n_acc[0] == n_acc[5] == -1
     run(tokens, parents, choices=p.argmax(-1).to(torch.int32), n_new=n_new)
 
 
-def test_trees_that_are_none():
+@pytest.mark.parametrize("V", [50, 66000])
+def test_trees_that_are_none(V):
     # entries that name no earlier node, several nodes of one token, tokens outside the vocabulary
-    tokens, parents, p, u = inputs(8, 30, 50, sharp=6.0)
+    tokens, parents, p, u = inputs(8, 30, V, sharp=6.0)
     parents[0, 5:], parents[1, 7], parents[2, 3], parents[3] = -1, 7, 29, 0
     parents[4, 0], parents[5, 0], parents[6, 9] = 3, 2 ** 31 - 1, -2 ** 31
     tokens[3] = tokens[3, 1]
-    tokens[4, ::2], tokens[5, ::3], tokens[6, 4] = -1, 50, 2 ** 31 - 1
+    tokens[4, ::2], tokens[5, ::3], tokens[6, 4] = -1, V, 2 ** 31 - 1
     run(tokens, parents, p, u)
 
 
-def test_weights_that_are_none():
-    tokens, parents, p, u = inputs(6, 10, 400)
+@pytest.mark.parametrize("dtype", [FP, BF])
+@pytest.mark.parametrize("V", [400, 3472, 66000])
+def test_weights_that_are_none(dtype, V):
+    # at every place of a load
+    tokens, parents, p, u = inputs(16, 4, V, dtype)
+    for b in range(16):
+        p[b, 0, b], p[b, 1:, V - 1 - b] = (math.inf, math.nan, -2.0, -math.inf)[b % 4], math.inf
+    run(tokens, parents, p, u)
+    tokens, parents, p, u = inputs(6, 10, V, dtype)
     p[0], p[1, 0], p[2, 0, 7], p[3, 0, 5], p[4, :, 100:] = 0.0, -0.5, math.nan, math.inf, 0.0
     tokens[0] = -1                                             # a draw of -1 is no node's token
     run(tokens, parents, p, u)
@@ -123,7 +132,7 @@ def test_kept_tokens_follow_the_targets_distribution():
     assert bool(((counts - B * want).abs() <= 5 * (B * want * (1 - want)).sqrt()).all())
 
 
-@pytest.mark.parametrize("B,N,V", [(1, 26, 32000), (40, 12, 5000)])
+@pytest.mark.parametrize("B,N,V", [(1, 26, 32000), (40, 12, 5000), (2, 12, 70000)])
 def test_streams_and_replayed_graphs(B, N, V):
     tokens, parents, p, u = inputs(B, N, V)
     streams, graphs = [torch.cuda.Stream() for _ in range(2)], []

@@ -68,7 +68,7 @@ def test_attentions_that_are_refused(over, fragment):
     (dict(alt=None), "beside top"), (dict(dtype=7), "dtype"), (dict(token_bytes=2), "token_bytes"), (dict(B=0), "B >= 1"), (dict(T=0), "T >= 1"), (dict(V=0), "V >= 1"),
     (dict(strides=(-1, 1)), "strides"), (dict(strides=(1, -1)), "strides"), (dict(temperature=0.0), "temperature"), (dict(temperature=-1.0), "temperature"),
     (dict(temperature=math.nan), "temperature"), (dict(temperature=math.inf), "temperature"), (dict(temperature=1e-7), "temperature"), (dict(top=-1), "top"),
-    (dict(V=30000, ws=None), "workspace"), (dict(V=30000, nbytes=8), "workspace"), (dict(V=30000, ws=PTR + 4), "workspace"),
+    (dict(V=100000, ws=None), "workspace"), (dict(V=100000, nbytes=8), "workspace"), (dict(V=100000, ws=PTR + 4), "workspace"),
 ])
 def test_scores_that_are_refused(over, fragment):
     assert scores(**over) == BAD and fragment in said()
@@ -111,10 +111,11 @@ def test_workspaces():
     assert L.tsd_window_attn_workspace(C.byref(cache()), 1, 1, 4, 100, 10, 0, None) == BAD
     assert L.tsd_tree_attn_workspace(C.byref(cache()), 1, 1, 4, 100, 10, 0, None) == BAD
     assert L.tsd_token_logprobs_workspace(1000, 1, 32000, 5, C.byref(n)) == 0 and n.value == 0
-    for rows_, V, top in ((1, 32000, 5), (1, 1 << 23, 32), (700, 1 << 23, 0)):
+    for rows_, V, top in ((1, 131072, 5), (1, 1 << 23, 32), (700, 1 << 23, 0)):
         assert L.tsd_token_logprobs_workspace(rows_, 1, V, top, C.byref(n)) == 0 and rows_ * 2 * (24 + 8 * top) <= n.value <= rows_ * 32 * (24 + 8 * top)
     assert L.tsd_token_logprobs_workspace(1, 1, 100, 0, None) == BAD
-    assert L.tsd_verify_tree_workspace(3, 20, 32000, tsd.TSD_BF16, C.byref(n)) == 0
+    assert L.tsd_verify_tree_workspace(3, 20, 32000, tsd.TSD_BF16, C.byref(n)) == 0 and n.value == 0
+    assert L.tsd_verify_tree_workspace(3, 20, 131072, tsd.TSD_BF16, C.byref(n)) == 0 and n.value == 3 * 20 * 4
     assert L.tsd_verify_tree_workspace(3, 20, 32000, tsd.TSD_BF16, None) == BAD
 
 
