@@ -190,14 +190,37 @@ __device__ __forceinline__ long attn_key_row(const PagedAttnP& p, const AttnWork
   return place < w.key1 ? paged_row(p.cache, entry, attn_key<M>(w, place)) : -1;
 }
 
-// The parents of a sequence's nodes into LDS, -1 where an entry names no earlier node.  For a whole workgroup, which waits.
-__device__ __forceinline__ void attn_parents(const PagedAttnP& p, const AttnWork& w, short* parents) {
-  for (int i = threadIdx.x; i < w.n_new; i += blockDim.x) {
-    const int x = p.parents[(long)w.b * p.parents_stride + i];
-    parents[i] = (unsigned)x < (unsigned)i ? (short)x : (short)-1;
+// A lane's share of the parents of a sequence's nodes, asked for before the lengths are there.
+template <int M>
+struct AttnParents {
+  __device__ __forceinline__ AttnParents(const PagedAttnP&, const AttnWork&) {}
+};
+template <>
+struct AttnParents<kTree> {
+  int first, rest[kTreeNodes / 64 - 1];
+  __device__ __forceinline__ AttnParents(const PagedAttnP& p, const AttnWork& w) {
+    const int* from = p.parents + (long)w.b * p.parents_stride;
+    first = from[min((int)threadIdx.x, p.T - 1)];
+#pragma unroll
+    for (int i = 0; i < kTreeNodes / 64 - 1; ++i) {
+      const int n = threadIdx.x + (i + 1) * blockDim.x;
+      rest[i] = n < p.T ? from[n] : -1;
+    }
   }
-  __syncthreads();
-}
+  // Into LDS, -1 where an entry names no earlier node.  For a whole workgroup, which waits.
+  __device__ __forceinline__ void put(const PagedAttnP& p, short* parents) const {
+    const auto one = [&](int n, int x) {
+      if (n < p.T) parents[n] = (unsigned)x < (unsigned)n ? (short)x : (short)-1;
+    };
+    one(threadIdx.x, first);
+#pragma unroll
+    for (int i = 0; i < kTreeNodes / 64 - 1; ++i) one(threadIdx.x + (i + 1) * blockDim.x, rest[i]);
+    __syncthreads();
+  }
+};
+// Whether the workgroup's keys are seen by what nodes are: there are nodes among them, or windows to begin somewhere.
+__device__ __forceinline__ bool attn_needs_lines(const PagedAttnP& p, const AttnWork& w) { return w.key1 > w.held || p.window < w.len; }
+
 // A node's line: itself and those of its ancestors that it sees.  Returns its depth.  (Parents come before their children: it ends.)
 __device__ __forceinline__ int attn_line(const PagedAttnP& p, const AttnWork& w, const short* parents, int node, uint64_t (&line)[kTreeNodes / 64]) {
   constexpr int N = kTreeNodes / 64;
@@ -230,9 +253,10 @@ struct AttnLines {
   short parents[kTreeNodes];
   short depth[kLineTokens + 1];
 };
-__device__ __forceinline__ void attn_lines(const PagedAttnP& p, const AttnWork& w, int tile_rows, AttnLines& l) {
-  attn_parents(p, w, l.parents);
-  const int t0 = w.row0 / p.G, n = (min(w.rows, w.row0 + tile_rows) - 1) / p.G - t0 + 1;
+__device__ __forceinline__ void attn_lines(const PagedAttnP& p, const AttnWork& w, const AttnParents<kTree>& parents, int tile_rows, AttnLines& l) {
+  const bool needed = attn_needs_lines(p, w);
+  if (needed) parents.put(p, l.parents);
+  const int t0 = w.row0 / p.G, n = needed ? (min(w.rows, w.row0 + tile_rows) - 1) / p.G - t0 + 1 : 0;
   for (int i = threadIdx.x; i <= kLineTokens; i += blockDim.x) {
     uint64_t line[kTreeNodes / 64] = {};
     l.depth[i] = i < n ? (short)attn_line(p, w, l.parents, t0 + i, line) : (short)0;
@@ -241,10 +265,14 @@ __device__ __forceinline__ void attn_lines(const PagedAttnP& p, const AttnWork& 
   }
   __syncthreads();
 }
-__device__ __forceinline__ AttnSight attn_tree_sight(const PagedAttnP& p, const AttnWork& w, const AttnLines& l, int row) {
-  if (row >= w.rows) return {0, 0, l.line[kLineTokens]};
-  const int i = row / p.G - w.row0 / p.G;
-  return attn_node_sight(p, w, l.depth[i], l.line[i]);
+// Which of a tile's lines a row has, and what it sees by that.
+__device__ __forceinline__ int attn_line_at(const PagedAttnP& p, const AttnWork& w, int row) {
+  return row < w.rows ? row / p.G - w.row0 / p.G : kLineTokens;
+}
+__device__ __forceinline__ AttnSight attn_line_sight(const PagedAttnP& p, const AttnWork& w, const AttnLines& l, int at) {
+  AttnSight a = attn_node_sight(p, w, l.depth[at], l.line[at]);
+  if (at == kLineTokens) a.sees = 0;
+  return a;
 }
 
 // One step of the running softmax of a row: its lanes (q, q + 16, q + 32, q + 48) hold 8 scores each, in base 2 and -inf where the row does not

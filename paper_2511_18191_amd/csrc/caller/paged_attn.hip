@@ -33,24 +33,29 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
   const int stride = 32 * waves;
   int sb = w.key0 + 32 * wave;
   // (lane i and lane i + 32: key i of a step)
-  int entry, next_entry;
-  if constexpr (M == kCausal) {  // (the table's entries are on their way before the lengths are there)
-    entry = paged_entry(p.cache, table, sb + (lane & 31));
-    next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
-  }
+  // (the table's entries are on their way before the lengths are there: nearly always places are keys)
+  int entry = paged_entry(p.cache, table, sb + (lane & 31)), next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
+  const AttnParents<M> parents(p, w);
   attn_lengths<M>(p, w, 16 * MT);
   if (w.idle) return;
-  if constexpr (M != kCausal) {
+  if (M != kCausal && w.gap) {
     entry = attn_entry<M>(p, w, table, sb + (lane & 31));
     next_entry = attn_entry<M>(p, w, table, sb + stride + (lane & 31));
   }
   __shared__ std::conditional_t<M == kTree, AttnLines, int> lines;
-  if constexpr (M == kTree) attn_lines(p, w, 16 * MT, lines);
+  if constexpr (M == kTree) attn_lines(p, w, parents, 16 * MT, lines);
+  // (what a row sees; of nodes only where it is, in registers)
   const auto sight = [&](int row) {
     if constexpr (M == kTree)
-      return attn_tree_sight(p, w, lines, row);
+      return attn_line_at(p, w, row);
     else
       return attn_sight<M>(p, w, row);
+  };
+  const auto seen = [&](auto by, int from) {
+    if constexpr (M == kTree)
+      return attn_seen<M>(p, w, attn_line_sight(p, w, lines, by), from);
+    else
+      return attn_seen<M>(p, w, by, from);
   };
   const bf16* kbase = reinterpret_cast<const bf16*>(p.cache.k) + w.hk * p.cache.head_stride;
   const bf16* vbase = reinterpret_cast<const bf16*>(p.cache.v) + w.hk * p.cache.head_stride;
@@ -58,7 +63,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
   const bf16x8 zero = {};
 
   bf16x8 qf[MT][KK];
-  AttnSight sees[MT];
+  decltype(sight(0)) sees[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int row = w.row0 + mt * 16 + qi;
@@ -129,7 +134,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
     const long later = attn_key_row<M>(p, w, entry, sb + 2 * stride + (lane & 31));
     entry = attn_entry<M>(p, w, table, sb + 3 * stride + (lane & 31));
     const bool whole = valid == 0xFFFFFFFFu && attn_all_see<M>(p, w, sb, 32);  // every row of the tile sees every key
+    unsigned live[MT] = {};  // of the lane's 8 keys
     if (!whole) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        if constexpr (M == kCausal)
+          live[mt] = (valid & attn_bits(sees[mt].sees - sb)) >> (8 * g);
+        else
+          live[mt] = (valid & seen(sees[mt], sb)) >> (8 * g);
+      }
       // keys that are not there hold anything; their weights are 0, and so must the values be
 #pragma unroll
       for (int i = 0; i < NV; ++i)
@@ -166,10 +179,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] = sc[mt][j >> 2][j & 3] * p.scale2;
       if (!whole) {
-        const unsigned live = (M == kCausal ? valid : valid & attn_seen<M>(p, w, sees[mt], sb)) >> (8 * g);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (!(live >> j & 1) || (M == kCausal && sb + 8 * g + j >= sees[mt].sees)) s[j] = -INFINITY;
+          if (!(live[mt] >> j & 1)) s[j] = -INFINITY;
       }
       const float alpha = attn_running_max(s, m_run[mt], e);
       float sum = 0.f;
@@ -204,15 +216,19 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
     }
   }
   if (__any(odd)) {
-    const auto reaches = [&](int key, int mt, int r) {
-      if constexpr (M == kCausal)
-        return key < __shfl(sees[mt].sees, 4 * g + r);
-      else
-        return bool(attn_seen<M>(p, w, sight(w.row0 + mt * 16 + 4 * g + r), key) & 1);
-    };
     for (int key = attn_mixed_from<M>(w, 32); key < w.key1; ++key) {
       const long at = attn_key_row<M>(p, w, attn_entry<M>(p, w, table, key), key);
       if (at < 0 || (key - w.key0) / 32 % waves != wave || (M != kCausal && !attn_mixed<M>(p, w, key - (key - w.key0) % 32, 32))) continue;
+      unsigned reached = 0;  // (by the lane's rows)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (M == kCausal)
+            reached |= key < __shfl(sees[mt].sees, 4 * g + r) ? 1u << (4 * mt + r) : 0u;
+          else
+            reached |= (seen(sight(w.row0 + mt * 16 + 4 * g + r), key) & 1) << (4 * mt + r);
+        }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const float v = FULL || nb * 16 + qi < p.D ? attn_taken((float)vbase[at + nb * 16 + qi]) : 0.f;
@@ -220,7 +236,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (reaches(key, mt, r)) o[mt][nb][r] += v;
+            if (reached >> (4 * mt + r) & 1) o[mt][nb][r] += v;
       }
     }
   }
@@ -341,7 +357,12 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3), and not for many rows (2 chunks of 128 rows of 64 24.5 and 15.4).
 // Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys
 // 45.9 us, two 46.8, four 52.0).
-// All of this goes by the places that a row tile may have, where windows leave fewer of them than max_len.
+// All of this goes by the places that a row tile may have, where windows leave fewer of them than max_len.  Windows make lengths alike, and a tree's rows are
+// many to join: their chunks are longer.  Few rows (us with 1024, 3072 keys and whole): 64 tokens at a window of 4096, 32 heads over 8 of 128, 191, 190, 179,
+// 32 100, 96, 90, but 16 (2048) 53, 52, 66; trees of 8 nodes over up to 16384 keys, 16 sequences 154, 146, 143 (8192), up to 3000 keys, 64 sequences 136, 121, 121; of
+// 64, 16 heads of 64, 296, 261, 246 (4096).  Trees of many rows: chunks for some 1024 workgroups, as the lengths leave half of them idle, but 2048 keys
+// where tiles alone fill the card: 64 nodes over up to 16384 keys, 32 heads over 8 of 128, 16 sequences whole 446, 8192 343, 4096 317, 2048 307, 1024 366, 4
+// sequences 4096 133, 2048 99, 1024 104, 512 117, 1 sequence 1024 46, 256 39; up to 2000 keys, 16 sequences, whole 68, 1024 74, 512 79.
 struct AttnPlan {
   bool prompt;  // the kernel for many rows
   int mt, waves, row_tiles, splits, chunk, reach;
@@ -375,10 +396,15 @@ AttnPlan attn_plan(const AttnAsk& ask, int dtype, int B, int T, int Hq, int Hkv,
   int64_t chunk = max_len;
   const bool tall = a.prompt && a.row_tiles > 1;  // (sums of many rows cost more to join than unequal lengths do)
   if (base < (tall ? 256 : 1024)) {
-    chunk = std::min<int64_t>(max_len * base / 256, tall ? max_len : 1024);
+    const int64_t most = tall ? max_len : ask.mask == kCausal ? 1024 : max_len <= 4608 ? max_len : 3072;
+    chunk = std::min<int64_t>(max_len * base / 256, most);
     chunk = chunk < step + step / 4 ? step : (chunk + step - 1) / step * step;
   }
-  if (a.prompt) chunk = std::max(chunk, max_len <= 256 ? 256 : std::min<int64_t>(256, (max_len + 511) / 512 * 64));
+  // (many rows: not less than is worth joining)
+  const int64_t least = !a.prompt ? 1 : max_len <= 256 ? 256 : std::min<int64_t>(256, (max_len + 511) / 512 * 64);
+  if (a.prompt && ask.mask == kTree) chunk = std::max<int64_t>(max_len * base / 1024, base >= 256 ? 2048 : std::min(8 * base, (int64_t)max_len / 4));
+  chunk = std::max(chunk, least);
+  if (ask.mask != kCausal && max_len - chunk < chunk / 4) chunk = max_len;
   chunk = std::min<int64_t>(std::max(chunk, max_len * base / 16384), max_len);  // (a sequence that stays whole: no longer than it is)
   chunk = (chunk + step - 1) / step * step;
   a.chunk = (int)chunk;

@@ -23,31 +23,36 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
   const int stride = 32 * waves;
   int sb = w.key0 + 32 * wave;
   // (lane i and lane i + 32: key i of a step)
-  int entry, next_entry;
-  if constexpr (M == kCausal) {  // (the table's entries are on their way before the lengths are there)
-    entry = paged_entry(p.cache, table, sb + (lane & 31));
-    next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
-  }
+  // (the table's entries are on their way before the lengths are there: nearly always places are keys)
+  int entry = paged_entry(p.cache, table, sb + (lane & 31)), next_entry = paged_entry(p.cache, table, sb + stride + (lane & 31));
+  const AttnParents<M> parents(p, w);
   attn_lengths<M>(p, w, 16 * MT);
   if (w.idle) return;
-  if constexpr (M != kCausal) {
+  if (M != kCausal && w.gap) {
     entry = attn_entry<M>(p, w, table, sb + (lane & 31));
     next_entry = attn_entry<M>(p, w, table, sb + stride + (lane & 31));
   }
   __shared__ std::conditional_t<M == kTree, AttnLines, int> lines;
-  if constexpr (M == kTree) attn_lines(p, w, 16 * MT, lines);
+  if constexpr (M == kTree) attn_lines(p, w, parents, 16 * MT, lines);
+  // (what a row sees; of nodes only where it is, in registers)
   const auto sight = [&](int row) {
     if constexpr (M == kTree)
-      return attn_tree_sight(p, w, lines, row);
+      return attn_line_at(p, w, row);
     else
       return attn_sight<M>(p, w, row);
+  };
+  const auto seen = [&](auto by, int from) {
+    if constexpr (M == kTree)
+      return attn_seen<M>(p, w, attn_line_sight(p, w, lines, by), from);
+    else
+      return attn_seen<M>(p, w, by, from);
   };
   const float* kbase = reinterpret_cast<const float*>(p.cache.k) + w.hk * p.cache.head_stride;
   const float* vbase = reinterpret_cast<const float*>(p.cache.v) + w.hk * p.cache.head_stride;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
   f32x4 qf[MT][KC];
-  AttnSight sees[MT];
+  decltype(sight(0)) sees[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int row = w.row0 + mt * 16 + qi;
@@ -141,12 +146,16 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float s[8];
-      const unsigned live = M == kCausal || whole ? valid : valid & attn_seen<M>(p, w, sees[mt], sb);
+      unsigned live = valid;
+      if constexpr (M == kCausal)
+        live &= attn_bits(sees[mt].sees - sb);
+      else if (!whole)
+        live &= seen(sees[mt], sb);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s[j] = sc[mt][j >> 2][j & 3] * p.scale2;
         const int key = 16 * (j >> 2) + 4 * g + (j & 3);
-        if (!whole && (!(live >> key & 1) || (M == kCausal && sb + key >= sees[mt].sees))) s[j] = -INFINITY;
+        if (!whole && !(live >> key & 1)) s[j] = -INFINITY;
       }
       const float alpha = attn_running_max(s, m_run[mt], e[mt]);
       float sum = 0.f;
@@ -180,15 +189,19 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
   }
 
   if (__any(odd)) {
-    const auto reaches = [&](int key, int mt, int r) {
-      if constexpr (M == kCausal)
-        return key < __shfl(sees[mt].sees, 4 * g + r);
-      else
-        return bool(attn_seen<M>(p, w, sight(w.row0 + mt * 16 + 4 * g + r), key) & 1);
-    };
     for (int key = attn_mixed_from<M>(w, 32); key < w.key1; ++key) {
       const long at = attn_key_row<M>(p, w, attn_entry<M>(p, w, table, key), key);
       if (at < 0 || (key - w.key0) / 32 % waves != wave || (M != kCausal && !attn_mixed<M>(p, w, key - (key - w.key0) % 32, 32))) continue;
+      unsigned reached = 0;  // (by the lane's rows)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (M == kCausal)
+            reached |= key < __shfl(sees[mt].sees, 4 * g + r) ? 1u << (4 * mt + r) : 0u;
+          else
+            reached |= (seen(sight(w.row0 + mt * 16 + 4 * g + r), key) & 1) << (4 * mt + r);
+        }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const f32x4 x = FULL || c * 64 + qi * 4 < p.D ? *reinterpret_cast<const f32x4*>(vbase + at + c * 64 + qi * 4) : zero;
@@ -198,7 +211,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              if (reaches(key, mt, r)) o[mt][c][j][r] += attn_taken(x[j]);
+              if (reached >> (4 * mt + r) & 1) o[mt][c][j][r] += attn_taken(x[j]);
       }
     }
   }

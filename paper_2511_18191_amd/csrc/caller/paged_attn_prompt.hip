@@ -36,14 +36,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
   AttnWork w = attn_place(p, WAVES * kWaveRows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r32 = lane & 31, h = lane >> 5;
   const int* table = p.cache.table + (long)w.b * p.cache.table_stride;
-  int entry, next_entry;
-  if constexpr (M == kCausal) {  // (the table's entries are on their way before the lengths are there)
-    entry = paged_entry(p.cache, table, w.key0 + lane);
-    next_entry = paged_entry(p.cache, table, w.key0 + kTile + lane);
-  }
+  // (the table's entries are on their way before the lengths are there: nearly always places are keys)
+  int entry = paged_entry(p.cache, table, w.key0 + lane), next_entry = paged_entry(p.cache, table, w.key0 + kTile + lane);
+  const AttnParents<M> parents(p, w);
   attn_lengths<M>(p, w, WAVES * kWaveRows);
   if (w.idle) return;
-  if constexpr (M != kCausal) {
+  if (M != kCausal && w.gap) {
     entry = attn_entry<M>(p, w, table, w.key0 + lane);
     next_entry = attn_entry<M>(p, w, table, w.key0 + kTile + lane);
   }
@@ -58,11 +56,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_prompt_kernel(const 
   AttnSight sees = attn_sight<M>(p, w, row);
   uint64_t line[kTreeNodes / 64] = {};
   if constexpr (M == kTree) {
-    short* parents = reinterpret_cast<short*>(smem);
-    attn_parents(p, w, parents);
     sees = {0, 0, line};
-    if (row < w.rows) sees = attn_node_sight(p, w, attn_line(p, w, parents, row / p.G, line), line);
-    __syncthreads();  // (the parents' place is the first tile's)
+    const bool needed = attn_needs_lines(p, w);
+    short* up = reinterpret_cast<short*>(smem);
+    if (needed) parents.put(p, up);
+    if (row < w.rows) sees = attn_node_sight(p, w, needed ? attn_line(p, w, up, row / p.G, line) : 0, line);
+    if (needed) __syncthreads();  // (the parents' place is the first tile's)
   }
   bf16x8 qf[KK];
   {
