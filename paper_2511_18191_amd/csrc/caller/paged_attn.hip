@@ -26,6 +26,7 @@ template <int M, int DP, int MT, bool FULL>  // M: AttnMask; FULL: head_dim is D
 __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn_bf16_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int KK = DP / 32, NB = DP / 16, VS = v_stride(DP), NV = DP / 16, VC = DP / 8;
+  constexpr int kSure = FULL ? DP : DP == 32 ? 8 : DP == 64 ? 40 : DP == 96 ? 72 : DP == 128 ? 104 : 136;  // dims that every head of this kernel has
   AttnWork w = attn_place(p, 16 * MT);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int qi = lane & 15, g = lane >> 4;
@@ -73,7 +74,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       const int d = kk * 32 + g * 8;
-      qf[mt][kk] = FULL || d < p.D ? *reinterpret_cast<const bf16x8*>(q + d) : zero;
+      qf[mt][kk] = kk * 32 + 32 <= kSure || d < p.D ? *reinterpret_cast<const bf16x8*>(q + d) : zero;
     }
   }
   f32x4 o[MT][NB];
@@ -101,8 +102,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 128 ? 2 : 1) void paged_attn
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
         const int d = kk * 32 + g * 8;
-        kf[bi][kk] = *reinterpret_cast<const bf16x8*>(k + (FULL || d < p.D ? d : 0));
-        if (!FULL && d >= p.D) kf[bi][kk] = zero;
+        const bool in = kk * 32 + 32 <= kSure || d < p.D;
+        kf[bi][kk] = *reinterpret_cast<const bf16x8*>(k + (in ? d : 0));
+        if (!in) kf[bi][kk] = zero;
       }
     }
   };
@@ -363,6 +365,8 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // 64, 16 heads of 64, 296, 261, 246 (4096).  Trees of many rows: chunks for some 1024 workgroups, as the lengths leave half of them idle, but 2048 keys
 // where tiles alone fill the card: 64 nodes over up to 16384 keys, 32 heads over 8 of 128, 16 sequences whole 446, 8192 343, 4096 317, 2048 307, 1024 366, 4
 // sequences 4096 133, 2048 99, 1024 104, 512 117, 1 sequence 1024 46, 256 39; up to 2000 keys, 16 sequences, whole 68, 1024 74, 512 79.
+// In fp32, where products bound, and of lengths that windows make alike, tiles of 16 rows fill the card better up to 128 rows: 51 rows at a window of 500, 24
+// sequences, 4 heads of 80 34 us against 37, of 128 32 and 43, 200 sequences 118 and 168, but 256 rows, 16 sequences, 8 heads of 128, 307 and 247.
 struct AttnPlan {
   bool prompt;  // the kernel for many rows
   int mt, waves, row_tiles, splits, chunk, reach;
@@ -383,7 +387,8 @@ AttnPlan attn_plan(const AttnAsk& ask, int dtype, int B, int T, int Hq, int Hkv,
   AttnPlan a;
   const int64_t rows = (int64_t)T * (Hq / Hkv);
   a.prompt = dtype == TSD_BF16 && D <= 128 && (rows > 64 || (rows > 32 && D > 96 && (int64_t)B * Hkv >= 64));
-  a.mt = rows <= 16 || D > 128 ? 1 : 2;
+  const bool small = ask.mask != kCausal && dtype == TSD_F32 && rows <= 128;
+  a.mt = rows <= 16 || D > 128 || small ? 1 : 2;
   const int tile_rows = a.prompt ? kPromptRows : 16 * a.mt;
   a.row_tiles = (int)((rows + tile_rows - 1) / tile_rows);
   // (the tokens that a tile's rows may belong to; a tree's nodes are at most as far apart as there are nodes)

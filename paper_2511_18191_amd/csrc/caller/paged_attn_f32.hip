@@ -5,17 +5,20 @@
 //   O += P V      lane (i, g) holds dims 4i .. 4i + 3 of every 64 of its key's row, one per instruction: no transposition.
 // One token of 64 sequences of 2000 keys, 32 heads over 8 of 128: 185 us, 5.7 TB/s; 16 over 4 of 256: 188 us, 5.6.  2 x 1024 tokens behind 2048, 32 heads
 // over 8 of 128: 934 us, 92 of the 148 TFLOP/s that a large product reaches: keys and values are fetched for every 32 rows; 16 over 4 of 256, where
-// registers spill (64 bytes of scratch a lane, 136 below 256 dims): 1051 us, 82.  Short calls are bound by the matrix instructions of a step, 128 of
-// 32 clocks for 80 dims as for 128, and three trips to memory.
+// registers spill (64 bytes of scratch a lane, 136 below 256 dims): 1051 us, 82.  Short calls are bound by the matrix instructions of a step, 104 of
+// 32 clocks for 80 dims, 128 for 128, and three trips to memory; heads of 80 and 96 dims have kernels of their own, two wavefronts of which share a SIMD
+// (3 tokens of 6 sequences of up to 1501 keys, 12 heads over 4 of 80: 17.2 us in the one for 128 dims, 16.0 so).
 #include "paged_attn.h"
 
 namespace tsd {
 namespace {
 
 template <int M, int DP, int MT, bool FULL>  // M: AttnMask; FULL: head_dim is DP
-__global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_f32_kernel(const PagedAttnP p) {
+__global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 || (DP <= 96 && MT == 1) ? 2 : 1) void paged_attn_f32_kernel(const PagedAttnP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  constexpr int KC = DP / 16, NC = DP / 64;
+  constexpr int KC = DP / 16, NC = (DP + 63) / 64;
+  constexpr bool kAll = FULL && NC * 64 == DP;  // every lane's dims of the values are there
+  constexpr int kSure = FULL ? DP : DP == 64 ? 8 : DP == 80 ? 72 : DP == 96 ? 88 : DP == 128 ? 104 : 136;  // dims that every head of this kernel has
   AttnWork w = attn_place(p, 16 * MT);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int qi = lane & 15, g = lane >> 4;
@@ -60,7 +63,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
     const int r = min(row, w.rows - 1), t = r / p.G, h = w.hk * p.G + r - t * p.G;
     const float* q = reinterpret_cast<const float*>(p.q.p) + w.b * p.q.sb + t * p.q.st + h * p.q.sh;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) qf[mt][c] = FULL || c * 16 + g * 4 < p.D ? *reinterpret_cast<const f32x4*>(q + c * 16 + g * 4) : zero;
+    for (int c = 0; c < KC; ++c) qf[mt][c] = c * 16 + 16 <= kSure || c * 16 + g * 4 < p.D ? *reinterpret_cast<const f32x4*>(q + c * 16 + g * 4) : zero;
   }
   f32x4 o[MT][NC][4];  // [..][j]: dim 64 c + 4 qi + j of rows 4g ..
   float m_run[MT], l_run[MT];
@@ -82,8 +85,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         const int d = c * 16 + g * 4;
-        kf[bi][c] = *reinterpret_cast<const f32x4*>(k + (FULL || d < p.D ? d : 0));
-        if (!FULL && d >= p.D) kf[bi][c] = zero;
+        const bool in = c * 16 + 16 <= kSure || d < p.D;
+        kf[bi][c] = *reinterpret_cast<const f32x4*>(k + (in ? d : 0));
+        if (!in) kf[bi][c] = zero;
       }
     }
   };
@@ -94,7 +98,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
       for (int r = 0; r < 4; ++r) {
         const float* v = vbase + __shfl(off, 16 * bi + 4 * g + r);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) vf[bi][r][c] = *reinterpret_cast<const f32x4*>(v + (FULL || c * 64 + qi * 4 < p.D ? c * 64 + qi * 4 : 0));  // (dims from D on: anything, never written)
+        for (int c = 0; c < NC; ++c) vf[bi][r][c] = *reinterpret_cast<const f32x4*>(v + (kAll || c * 64 + qi * 4 < p.D ? c * 64 + qi * 4 : 0));  // (dims from D on: anything, never written)
       }
   };
 
@@ -204,7 +208,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
         }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const f32x4 x = FULL || c * 64 + qi * 4 < p.D ? *reinterpret_cast<const f32x4*>(vbase + at + c * 64 + qi * 4) : zero;
+        const f32x4 x = kAll || c * 64 + qi * 4 < p.D ? *reinterpret_cast<const f32x4*>(vbase + at + c * 64 + qi * 4) : zero;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -231,7 +235,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 ? 2 : 1) void paged_attn_
           f32x4 y;
 #pragma unroll
           for (int j = 0; j < 4; ++j) y[j] = o[mt][c][j][r];
-          *reinterpret_cast<f32x4*>(to + (4 * g + r) * rs + c * 64 + qi * 4) = y;
+          if (NC * 64 == DP || c * 64 + qi * 4 < DP) *reinterpret_cast<f32x4*>(to + (4 * g + r) * rs + c * 64 + qi * 4) = y;
         }
     });
   }
@@ -253,6 +257,8 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 template <int M>
 hipError_t launch_mask(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
   if (p.D <= 64) return launch_dp<M, 64>(p, mt, waves, st);
+  if (p.D <= 80) return launch_dp<M, 80>(p, mt, waves, st);
+  if (p.D <= 96) return launch_dp<M, 96>(p, mt, waves, st);
   if (p.D <= 128) return launch_dp<M, 128>(p, mt, waves, st);
   return launch_dp<M, 256>(p, mt, waves, st);
 }
