@@ -4,8 +4,7 @@
 //                 lane (q, g) ends up with keys 4g .. 4g + 3 of each 16 for row q: the A operand of the next product, a key per instruction;
 //   O += P V      lane (i, g) holds dims 4i .. 4i + 3 of every 64 of its key's row, one per instruction: no transposition.
 // One token of 64 sequences of 2000 keys, 32 heads over 8 of 128: 185 us, 5.7 TB/s; 16 over 4 of 256: 188 us, 5.6.  2 x 1024 tokens behind 2048, 32 heads
-// over 8 of 128: 934 us, 92 of the 148 TFLOP/s that a large product reaches: keys and values are fetched for every 32 rows; 16 over 4 of 256, where
-// registers spill (64 bytes of scratch a lane, 136 below 256 dims): 1051 us, 82.  Short calls are bound by the matrix instructions of a step, 104 of
+// over 8 of 128: 934 us, 92 of the 148 TFLOP/s that a large product reaches: keys and values are fetched for every 32 rows; 16 over 4 of 256: 1051 us, 82.  Short calls are bound by the matrix instructions of a step, 104 of
 // 32 clocks for 80 dims, 128 for 128, and three trips to memory; heads of 80 and 96 dims have kernels of their own, two wavefronts of which share a SIMD
 // (3 tokens of 6 sequences of up to 1501 keys, 12 heads over 4 of 80: 17.2 us in the one for 128 dims, 16.0 so).
 #include "paged_attn.h"
@@ -54,7 +53,13 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 || (DP <= 96 && MT == 1) 
   const float* vbase = reinterpret_cast<const float*>(p.cache.v) + w.hk * p.cache.head_stride;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
-  f32x4 qf[MT][KC];
+  // Above 128 dims the queries stay in LDS: with them registers spilled, and a value of four that the compiler keeps half in matrix registers and half in
+  // memory came back without one of its parts (wrong scores; ROCm 7.2).
+  constexpr bool kStaged = DP > 128;
+  constexpr int QS = DP + 4;
+  static_assert(!kStaged || MT == 1);
+  float* staged = reinterpret_cast<float*>(smem);  // [16][QS], until the join takes the place
+  f32x4 qf[MT][kStaged ? 1 : KC];
   decltype(sight(0)) sees[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
@@ -63,8 +68,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 || (DP <= 96 && MT == 1) 
     const int r = min(row, w.rows - 1), t = r / p.G, h = w.hk * p.G + r - t * p.G;
     const float* q = reinterpret_cast<const float*>(p.q.p) + w.b * p.q.sb + t * p.q.st + h * p.q.sh;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) qf[mt][c] = c * 16 + 16 <= kSure || c * 16 + g * 4 < p.D ? *reinterpret_cast<const f32x4*>(q + c * 16 + g * 4) : zero;
+    for (int c = 0; c < KC; ++c) {
+      const f32x4 x = c * 16 + 16 <= kSure || c * 16 + g * 4 < p.D ? *reinterpret_cast<const f32x4*>(q + c * 16 + g * 4) : zero;
+      if constexpr (!kStaged)
+        qf[mt][c] = x;
+      else if (wave == 0)
+        *reinterpret_cast<f32x4*>(staged + qi * QS + c * 16 + g * 4) = x;
+    }
   }
+  if constexpr (kStaged) __syncthreads();
   f32x4 o[MT][NC][4];  // [..][j]: dim 64 c + 4 qi + j of rows 4g ..
   float m_run[MT], l_run[MT];
 #pragma unroll
@@ -128,10 +140,17 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 || (DP <= 96 && MT == 1) 
 #pragma unroll
       for (int bi = 0; bi < 2; ++bi) {
         sc[mt][bi] = zero;
+        if constexpr (kStaged) asm volatile("" ::: "memory");  // (read anew in every step, not kept)
 #pragma unroll
-        for (int c = 0; c < KC; ++c)
+        for (int c = 0; c < KC; ++c) {
+          f32x4 x;
+          if constexpr (kStaged)
+            x = *reinterpret_cast<const f32x4*>(staged + qi * QS + c * 16 + g * 4);
+          else
+            x = qf[mt][c];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) sc[mt][bi] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[bi][c][j], qf[mt][c][j], sc[mt][bi], 0, 0, 0);
+          for (int j = 0; j < 4; ++j) sc[mt][bi] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[bi][c][j], x[j], sc[mt][bi], 0, 0, 0);
+        }
       }
     if (more) load_k(off);
     if (!whole) {

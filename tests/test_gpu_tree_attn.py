@@ -132,7 +132,7 @@ def test_a_node_that_is_not_finite_reaches_only_its_line(dtype, T, Hq):
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
-@pytest.mark.parametrize("D", [8, 32, 72, 96, 120, 128, 136, 192, 256])
+@pytest.mark.parametrize("D", [8, 32, 72, 80, 88, 96, 104, 120, 128, 136, 160, 192, 200, 248, 256])
 def test_head_sizes(dtype, D):
     for T, lens in ((3, [50, 300]), (45, [45, 200])):
         run(*inputs(2, T, 3, 1, D, 16, dtype, lens), random_tree(2, T, D))

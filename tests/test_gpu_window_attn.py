@@ -129,7 +129,7 @@ def test_a_token_that_is_not_finite_reaches_only_those_that_see_it(dtype, T, Hq)
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
-@pytest.mark.parametrize("D", [8, 32, 72, 96, 120, 128, 136, 192, 256])
+@pytest.mark.parametrize("D", [8, 32, 72, 80, 88, 96, 104, 120, 128, 136, 160, 192, 200, 248, 256])
 def test_head_sizes(dtype, D):
     # few rows and many, one key head for three query heads
     for T, lens in ((2, [50, 300]), (45, [45, 400])):
