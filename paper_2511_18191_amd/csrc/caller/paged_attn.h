@@ -85,12 +85,15 @@ __device__ __forceinline__ AttnWork attn_place(const PagedAttnP& p, int tile_row
   const unsigned pairs = p.B * p.Hkv;
   const unsigned pair = i % pairs;
   i /= pairs;
-  w.split = i % p.splits;
-  w.tile = p.row_tiles - 1 - i / p.splits;
+  // A tree's row tiles all see the same keys: those of a chunk run side by side, so that the second finds them in that L2 (64 nodes over up to 16384 keys, 16
+  // sequences, 32 heads over 8 of 128, two tiles: 1030 MB read one tile after the other).
+  const unsigned turn = p.mask == kTree ? i / p.row_tiles : i / p.splits;
+  w.split = p.mask == kTree ? turn : i - turn * p.splits;
+  w.tile = p.row_tiles - 1 - (p.mask == kTree ? i - turn * p.row_tiles : turn);
   w.b = pair / p.Hkv;
   w.hk = pair - w.b * p.Hkv;
   // Workgroups 256 apart tend to share a compute unit: they take different sequences, whose lengths differ.
-  w.b = (w.b + i / p.splits / max(1u, 256 / pairs)) % p.B;
+  w.b = (w.b + turn / max(1u, 256 / pairs)) % p.B;
   w.row0 = w.tile * tile_rows;
   w.key0 = w.split * p.chunk;
   w.split_out = p.splits > 1;
