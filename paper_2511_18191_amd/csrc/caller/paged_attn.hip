@@ -362,9 +362,10 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // All of this goes by the places that a row tile may have, where windows leave fewer of them than max_len.  Windows make lengths alike, and a tree's rows are
 // many to join: their chunks are longer.  Few rows (us with 1024, 3072 keys and whole): 64 tokens at a window of 4096, 32 heads over 8 of 128, 191, 190, 179,
 // 32 100, 96, 90, but 16 (2048) 53, 52, 66; trees of 8 nodes over up to 16384 keys, 16 sequences 154, 146, 143 (8192), up to 3000 keys, 64 sequences 136, 121, 121; of
-// 64, 16 heads of 64, 296, 261, 246 (4096).  Trees of many rows: chunks for some 1024 workgroups, as the lengths leave half of them idle, but 2048 keys
-// where tiles alone fill the card: 64 nodes over up to 16384 keys, 32 heads over 8 of 128, 16 sequences whole 446, 8192 343, 4096 317, 2048 307, 1024 366, 4
-// sequences 4096 133, 2048 99, 1024 104, 512 117, 1 sequence 1024 46, 256 39; up to 2000 keys, 16 sequences, whole 68, 1024 74, 512 79.
+// 64, 16 heads of 64, 296, 261, 246 (4096).  Trees of many rows: chunks for some 512 workgroups, of at most 2560 keys, as
+// long as the tiles alone do not fill the card: 64 nodes over up to 16384 keys, 32 heads over 8 of 128, us with 512, 1024, 2048, 2752, 4096, 8192: 16 sequences 352, 307, 263,
+// 261, 297, 319; 4 sequences 109, 99, 92, 109, 135, 242; 2 sequences 62, 59, 75, 94, 132, 236; 1 sequence (256: 39) 41, 46, 72; 8 sequences of 16000 307, 258, 220,
+// 223, 210, 258; 32 sequences of up to 8000 410, 289, 275, 272, 299, 307; but 16 of up to 2000 79, 74, whole 68, 64 of up to 4096 444, 407, 386, whole 305.
 // In fp32, where products bound, and of lengths that windows make alike, tiles of 16 rows fill the card better up to 128 rows: 51 rows at a window of 500, 24
 // sequences, 4 heads of 80 34 us against 37, of 128 32 and 43, 200 sequences 118 and 168, but 256 rows, 16 sequences, 8 heads of 128, 307 and 247.
 struct AttnPlan {
@@ -407,7 +408,12 @@ AttnPlan attn_plan(const AttnAsk& ask, int dtype, int B, int T, int Hq, int Hkv,
   }
   // (many rows: not less than is worth joining)
   const int64_t least = !a.prompt ? 1 : max_len <= 256 ? 256 : std::min<int64_t>(256, (max_len + 511) / 512 * 64);
-  if (a.prompt && ask.mask == kTree) chunk = std::max<int64_t>(max_len * base / 1024, base >= 256 ? 2048 : std::min(8 * base, (int64_t)max_len / 4));
+  if (a.prompt && ask.mask == kTree) {
+    chunk = std::max<int64_t>(max_len * base / (base < 32 ? 1024 : 512), base >= 256 ? 2048 : std::min(8 * base, (int64_t)max_len / 4));
+    chunk = std::max(least, std::min(chunk, 2560 * std::max<int64_t>(1, base / 512)));
+    const int64_t parts = std::max<int64_t>(1, (max_len + chunk / 2) / chunk);  // (alike)
+    chunk = (max_len + parts - 1) / parts;
+  }
   chunk = std::max(chunk, least);
   if (ask.mask != kCausal && max_len - chunk < chunk / 4) chunk = max_len;
   chunk = std::min<int64_t>(std::max(chunk, max_len * base / 16384), max_len);  // (a sequence that stays whole: no longer than it is)

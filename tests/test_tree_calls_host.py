@@ -119,6 +119,21 @@ def test_workspaces():
     assert L.tsd_verify_tree_workspace(3, 20, 32000, tsd.TSD_BF16, None) == BAD
 
 
+@pytest.mark.parametrize("dtype", [tsd.TSD_BF16, tsd.TSD_F32])
+@pytest.mark.parametrize("B", [1, 3, 16, 100, 5000])
+def test_plans_of_all_sizes(dtype, B):
+    # every length, few rows and many: a plan is made, of parts that hold at least a step of keys each
+    n, c = C.c_size_t(), cache(dtype=dtype)
+    for T in (1, 8, 40, 64, 256):
+        for m in [*range(1, 140), 200, 255, 256, 257, 300, 511, 513, 1000, 1025, 2047, 2049, 4095, 5000, 16384, 100000, 1 << 20, 1 << 30]:
+            for w, sinks in ((0, 0), (1, 0), (70, 3), (5000, 64), (1 << 30, 1 << 30)):
+                for call in ([L.tsd_tree_attn_workspace] if w == 0 else [L.tsd_tree_attn_workspace, L.tsd_window_attn_workspace]):
+                    assert call(C.byref(c), B, T, 8, m, w, sinks, C.byref(n)) == 0
+                    places = min(m, sinks + w + T) if w else m
+                    assert n.value <= (places // 32 + 1) * B * (T * 8 * 65 * 4 + 4 * (T * 2 // 16 + 1) * 8) + 256
+                    assert places > 32 or n.value == 0
+
+
 z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype)
 i32, i64 = torch.int32, torch.int64
 ATTN = lambda: [z(2, 3, 4, 64), z(9, 16, 4, 64), z(9, 16, 4, 64), z(2, 4, dtype=i32), z(2, dtype=i32)]
