@@ -11,7 +11,9 @@
 // left.  One token of 64 sequences of 100 to 8192 keys, 32 heads over 8 of 128: 212 us for 254387 keys in all, 4.9 TB/s (a copy reaches 5.2, eight other
 // draws of lengths 195 to 237 us, 4.7 to 5.0); 16 heads over 4 of 256, 2000 keys each: 97 us, 5.4 TB/s; 7 tokens of 512 sequences
 // of 80 keys, 16 heads of 64: 44 us, 4.1 TB/s, a wavefront's three steps behind two trips for its lengths and pages; 5 tokens of one
-// sequence of 32768 keys, 32 heads over 8 of 128: 36.5 us, 3.7 TB/s, of which the join is 5 and the first and last trips some 6.
+// sequence of 32768 keys, 32 heads over 8 of 128: 36.5 us, 3.7 TB/s, of which the join is 5 and the first and last trips some 6.  Windows read what they leave
+// visible: one token of 64 sequences, of the last 4096 keys and the first four of up to 16384, 32 heads over 8 of 128, 179 us, 946 MB, 5.3 TB/s; of the last 1024
+// of one sequence of 20000 10.3 us, trips.
 #include <algorithm>
 #include <cmath>
 
@@ -360,8 +362,8 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys
 // 45.9 us, two 46.8, four 52.0).
 // All of this goes by the places that a row tile may have, where windows leave fewer of them than max_len.  Windows make lengths alike, and a tree's rows are
-// many to join: their chunks are longer.  Few rows (us with 1024, 3072 keys and whole): 64 tokens at a window of 4096, 32 heads over 8 of 128, 191, 190, 179,
-// 32 100, 96, 90, but 16 (2048) 53, 52, 66; trees of 8 nodes over up to 16384 keys, 16 sequences 154, 146, 143 (8192), up to 3000 keys, 64 sequences 136, 121, 121; of
+// many to join: their chunks are longer.  Few rows (us with 1024, some 3000 keys and whole): 64 tokens at a window of 4096, 32 heads over 8 of 128, 191, 190, 179,
+// 32 100, 96, 90, but 16 (2048) 53, 52, 66; trees of 8 nodes over up to 16384 keys, 16 sequences 154, 146 (2560: 140), 143 (8192), up to 3000 keys, 64 sequences 136, 121, 121; of
 // 64, 16 heads of 64, 296, 261, 246 (4096).  Trees of many rows: chunks for some 512 workgroups, of at most 2560 keys, as
 // long as the tiles alone do not fill the card: 64 nodes over up to 16384 keys, 32 heads over 8 of 128, us with 512, 1024, 2048, 2752, 4096, 8192: 16 sequences 352, 307, 263,
 // 261, 297, 319; 4 sequences 109, 99, 92, 109, 135, 242; 2 sequences 62, 59, 75, 94, 132, 236; 1 sequence (256: 39) 41, 46, 72; 8 sequences of 16000 307, 258, 220,
@@ -402,7 +404,7 @@ AttnPlan attn_plan(const AttnAsk& ask, int dtype, int B, int T, int Hq, int Hkv,
   int64_t chunk = max_len;
   const bool tall = a.prompt && a.row_tiles > 1;  // (sums of many rows cost more to join than unequal lengths do)
   if (base < (tall ? 256 : 1024)) {
-    const int64_t most = tall ? max_len : ask.mask == kCausal ? 1024 : max_len <= 4608 ? max_len : 3072;
+    const int64_t most = tall ? max_len : ask.mask == kCausal ? 1024 : max_len <= 4608 ? max_len : 2560;
     chunk = std::min<int64_t>(max_len * base / 256, most);
     chunk = chunk < step + step / 4 ? step : (chunk + step - 1) / step * step;
   }

@@ -3,10 +3,11 @@
 //   S^T = K Q^T   lane group g takes 4 consecutive dims in one load, one per instruction (which dims an instruction contracts is free);
 //                 lane (q, g) ends up with keys 4g .. 4g + 3 of each 16 for row q: the A operand of the next product, a key per instruction;
 //   O += P V      lane (i, g) holds dims 4i .. 4i + 3 of every 64 of its key's row, one per instruction: no transposition.
-// One token of 64 sequences of 2000 keys, 32 heads over 8 of 128: 185 us, 5.7 TB/s; 16 over 4 of 256: 188 us, 5.6.  2 x 1024 tokens behind 2048, 32 heads
-// over 8 of 128: 934 us, 92 of the 148 TFLOP/s that a large product reaches: keys and values are fetched for every 32 rows; 16 over 4 of 256: 1051 us, 82.  Short calls are bound by the matrix instructions of a step, 104 of
-// 32 clocks for 80 dims, 128 for 128, and three trips to memory; heads of 80 and 96 dims have kernels of their own, two wavefronts of which share a SIMD
-// (3 tokens of 6 sequences of up to 1501 keys, 12 heads over 4 of 80: 17.2 us in the one for 128 dims, 16.0 so).
+// One token of 64 sequences of 2000 keys, 32 heads over 8 of 128: 185 us, 5.7 TB/s; 16 over 4 of 256: 182 us, 5.8.  2 x 1024 tokens behind 2048, 32 heads
+// over 8 of 128: 934 us, 92 of the 148 TFLOP/s that a large product reaches: keys and values are fetched for every 32 rows; 16 over 4 of 256: 1049 us, 82.
+// Short calls are bound by the matrix instructions of a step, 104 of 32 clocks for 80 dims, 128 for 128, and three trips to memory; heads of 80 and 96 dims have kernels of their own, two wavefronts of which share a SIMD
+// (3 tokens of 6 sequences of up to 1501 keys, 12 heads over 4 of 80: 17.2 us in the one for 128 dims, 15.6 so;
+// trees of up to 17 nodes of 24 such sequences at a window of 500 34).
 #include "paged_attn.h"
 
 namespace tsd {
