@@ -83,6 +83,7 @@ extern "C" int tsd_keep_path_static(const tsd_paged_cache* cache, int32_t n_laye
   if (!held_dev || !path_dev) return fail_no_handle(TSD_E_INVALID_ARG, "held_dev and path_dev must not be NULL");
   const int es = type_bytes(cache->dtype);
   if (layer_stride < 0 || (layer_stride * es & 15)) return fail_no_handle(TSD_E_INVALID_ARG, "layer_stride must be a multiple of 16 bytes, not negative");
+  if (n_layers > 1 && !layer_stride) return fail_no_handle(TSD_E_INVALID_ARG, "layer_stride must not be 0 beside several layers: each would move the same rows");
   KeepP p;
   p.cache = cache_view(*cache);
   p.cache.page_stride *= es;

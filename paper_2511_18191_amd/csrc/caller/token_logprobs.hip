@@ -450,7 +450,8 @@ int check_scores(int32_t B, int32_t T, int32_t V, int32_t top) {
   if (top < 0) return fail_no_handle(TSD_E_INVALID_ARG, "top must not be negative");
   if (top > kMostTop) return fail_no_handle(TSD_E_OUT_OF_RANGE, "at most 32 alternatives");
   if (V > kMostTokensScored) return fail_no_handle(TSD_E_OUT_OF_RANGE, "V beyond 2^23");
-  if ((int64_t)B * T > max_workgroups(kLanes) / kMostGroups) return fail_no_handle(TSD_E_OUT_OF_RANGE, "B * T beyond what a launch takes");
+  const int64_t rows = (int64_t)B * T;
+  if (rows > max_workgroups(kLanes) || rows * score_plan(rows, V).groups > max_workgroups(kLanes)) return fail_no_handle(TSD_E_OUT_OF_RANGE, "B * T beyond what a launch takes");
   return TSD_OK;
 }
 

@@ -41,6 +41,16 @@ def test_many_rows(dtype, B, T, V, top):
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
+def test_very_many_rows(dtype):
+    # the same rows over and over
+    logits, tokens = inputs(5, 100, 37, dtype)
+    some = run(logits, tokens, 3)
+    all_of = tsd.token_logprobs_static(logits.repeat(110, 10, 1), tokens.repeat(110, 10), top=3)
+    for name, x in some.items():
+        assert torch.equal(all_of[name], x.repeat(110, 10, *[1] * (x.dim() - 2))), name
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("temperature", [0.05, 0.7, 1.3, 100.0])
 def test_temperatures(dtype, temperature):
     run(*inputs(2, 3, 5000, dtype), 4, temperature)

@@ -75,6 +75,15 @@ def test_scores_that_are_refused(over, fragment):
     assert scores(top=33) == RANGE and scores(V=(1 << 23) + 1) == RANGE and scores(B=1 << 15, T=1 << 15) == RANGE
 
 
+def test_scores_of_as_many_rows_as_a_launch_takes():
+    n = C.c_size_t(1)
+    most = 0xFFFFFFFF // 256  # workgroups of 256 lanes: one a row of up to 262144 logits
+    for B, T, V, rc in ((most, 1, 32000, 0), (1024, 4096, 32000, 0), (most + 1, 1, 32000, RANGE), (1 << 30, 1 << 30, 8, RANGE), (most // 2, 1, 262145, 0),
+                        (most // 2 + 1, 1, 262145, RANGE)):
+        assert L.tsd_token_logprobs_workspace(B, T, V, 5, C.byref(n)) == rc
+        assert rc or (n.value == 0) == (V <= 262144)
+
+
 @pytest.mark.parametrize("over,fragment", [
     (dict(tokens=None), "NULL"), (dict(parents=None), "NULL"), (dict(n_acc=None), "NULL"), (dict(out=None), "NULL"), (dict(path=None), "NULL"), (dict(p=None), "either"),
     (dict(choices=PTR), "either"), (dict(u=None), "uniforms"), (dict(dtype=5), "dtype"), (dict(token_bytes=1), "token_bytes"), (dict(stride=4), "parents_stride"),
@@ -88,11 +97,11 @@ def test_walks_that_are_refused(over, fragment):
 
 @pytest.mark.parametrize("over,fragment", [
     (dict(B=0), "B >= 1"), (dict(N=0), "N >= 1"), (dict(layers=0), "n_layers"), (dict(held=None), "NULL"), (dict(path=None), "NULL"), (dict(layers=2, stride=4), "layer_stride"),
-    (dict(layers=2, stride=-8), "layer_stride"),
+    (dict(layers=2, stride=-8), "layer_stride"), (dict(layers=2, stride=0), "layer_stride"),
 ])
 def test_kept_paths_that_are_refused(over, fragment):
     assert keep(**over) == BAD and fragment in said()
-    assert keep(N=257) == RANGE and keep(B=1 << 20, layers=1 << 10) == RANGE
+    assert keep(N=257) == RANGE and keep(B=1 << 20, layers=1 << 10, stride=4096) == RANGE
 
 
 def test_workspaces():
