@@ -2,7 +2,8 @@
 //
 // With d_v = (x_v - m) / temperature, m a maximum so far: S = sum e^d, W = sum d e^d; a larger m' takes them to f S and f (W + S (m - m') / temperature),
 // f = e^((m - m') / temperature).  Then log p_v = d_v - ln S and the entropy is ln S - W / S, two numbers that are not negative: nothing cancels.  (Differences to
-// the maximum itself are taken before the factor: logits may be as large as their type's largest.)
+// the maximum itself are taken before the factor: logits may be as large as their type's largest.  They are taken of quarters, and the factor is four times
+// as large: so are the temperatures, and neither the difference nor the factor leaves the normal numbers.  Quarters round as the whole do: same bits.)
 //
 // One pass over the row.  For the alternatives each lane's maxima of kCell elements stay in LDS.  A bound that at least `top` elements reach is had
 // by counting: of the maxima of all lanes, in fours, it is the top-th.  Only cells that reach it are read again (some
@@ -37,7 +38,7 @@ struct ScoreP {
   const void* tokens;  // int32 or int64 [B][T], or NULL
   const int* n_new;
   int B, T, V, top, wide;
-  float inv, scale2;   // 1 / temperature, and times log2 e
+  float inv4, scale4;  // 4 / temperature, and times log2 e (of quarters: base e, base 2)
   float *logprobs, *entropy, *top_logprobs;
   int* top_ids;
   int groups, per;     // workgroups of a row, and the elements that each of them takes
@@ -53,13 +54,16 @@ struct Sums {
 };
 constexpr Sums kNoSums = {-INFINITY, 0.f, 0.f};
 
-// What sums relative to `from` change by, relative to `to` >= from: the factor's exponent.
-__device__ __forceinline__ float shift_of(float from, float to, float scale2) { return from == -INFINITY ? 0.f : (from - to) * scale2; }
+// A quarter of a difference.
+__device__ __forceinline__ float quarter(float a, float b) { return fmaf(a, 0.25f, -0.25f * b); }
 
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float scale2) {
+// What sums relative to `from` change by, relative to `to` >= from: the factor's exponent.
+__device__ __forceinline__ float shift_of(float from, float to, float scale4) { return from == -INFINITY ? 0.f : quarter(from, to) * scale4; }
+
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float scale4) {
   Sums r;
   r.m = fmaxf(a.m, b.m);
-  const float da = shift_of(a.m, r.m, scale2), db = shift_of(b.m, r.m, scale2);
+  const float da = shift_of(a.m, r.m, scale4), db = shift_of(b.m, r.m, scale4);
   const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
   r.s = fa * a.s + fb * b.s;
   r.w = fa * fmaf(a.s, fmaxf(da, -200.f), a.w) + fb * fmaf(b.s, fmaxf(db, -200.f), b.w);
@@ -79,18 +83,18 @@ __device__ __forceinline__ unsigned index_of(uint64_t key) { return ~(unsigned)k
 
 // N elements x[] of a lane into its sums.  Returns the largest.
 template <int N>
-__device__ __forceinline__ float take(Sums& a, const float (&x)[N], float scale2) {
+__device__ __forceinline__ float take(Sums& a, const float (&x)[N], float scale4) {
   float mx = x[0];
 #pragma unroll
   for (int j = 1; j < N; ++j) mx = fmaxf(mx, x[j]);
   const float m = fmaxf(a.m, mx), from = m == -INFINITY ? 0.f : m;
-  const float d = shift_of(a.m, m, scale2), f = __builtin_amdgcn_exp2f(d);
+  const float d = shift_of(a.m, m, scale4), f = __builtin_amdgcn_exp2f(d);
   a.w = f * fmaf(a.s, fmaxf(d, -200.f), a.w);
   a.s *= f;
   a.m = m;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const float t = (x[j] - from) * scale2, e = __builtin_amdgcn_exp2f(t);  // (a NaN, or an infinite maximum, makes S a NaN)
+    const float t = quarter(x[j], from) * scale4, e = __builtin_amdgcn_exp2f(t);  // (a NaN, or an infinite maximum, makes S a NaN)
     a.s += e;
     a.w = fmaf(e, fmaxf(t, -200.f), a.w);  // (e is 0 there, and t may be infinite)
   }
@@ -285,14 +289,14 @@ __device__ __forceinline__ void find_top(const Part<T>& q, long base, const floa
 __device__ __forceinline__ void put_row(const ScoreP& a, long row, const Sums& z, float x, bool there) {
   const bool none = z.s == 0.f;  // no token weighs anything
   const float ln_s = logf(z.s);
-  if (a.logprobs) a.logprobs[row] = none || !there ? (z.s != z.s ? z.s : -INFINITY) : (x - z.m) * a.inv - ln_s;
+  if (a.logprobs) a.logprobs[row] = none || !there ? (z.s != z.s ? z.s : -INFINITY) : quarter(x, z.m) * a.inv4 - ln_s;
   a.entropy[row] = none ? 0.f : ln_s - z.w / z.s * 0.69314718055994531f;
 }
 // The likeliest of the keys in LDS.
 __device__ __forceinline__ void put_top(const ScoreP& a, long row, const Sums& z, const Candidates& f) {
   rank_keys(f.keys, f.n_found, a.top, [&](int rank, uint64_t key) {
     a.top_ids[row * a.top + rank] = (int)index_of(key);
-    a.top_logprobs[row * a.top + rank] = (value_of(key) - z.m) * a.inv - logf(z.s);
+    a.top_logprobs[row * a.top + rank] = quarter(value_of(key), z.m) * a.inv4 - logf(z.s);
   });
   if (threadIdx.x >= f.n_found && threadIdx.x < a.top) {
     a.top_ids[row * a.top + threadIdx.x] = -1;
@@ -337,7 +341,7 @@ __global__ __launch_bounds__(kLanes) void token_logprobs_kernel(const ScoreP a) 
       if (q.start(i, c0, 0) >= q.n) break;
       float x[N];
       load_cells<T, U>(q, i, c0, x);
-      cell = fmaxf(cell, take(z, x, a.scale2));
+      cell = fmaxf(cell, take(z, x, a.scale4));
     }
     if (TOP) maxima[i * kLanes + threadIdx.x] = cell;
   }
@@ -348,13 +352,13 @@ __global__ __launch_bounds__(kLanes) void token_logprobs_kernel(const ScoreP a) 
     y.m = __shfl_xor(z.m, o);
     y.s = __shfl_xor(z.s, o);
     y.w = __shfl_xor(z.w, o);
-    z = join(z, y, a.scale2);
+    z = join(z, y, a.scale4);
   }
   if (lane == 0) parts[wave] = z;
   __syncthreads();
   z = parts[0];
 #pragma unroll
-  for (int v = 1; v < kLanes / 64; ++v) z = join(z, parts[v], a.scale2);
+  for (int v = 1; v < kLanes / 64; ++v) z = join(z, parts[v], a.scale4);
   if constexpr (TOP) find_top(q, base, maxima, blocks, lane_max, a.top, found);
 
   if (a.groups == 1) {
@@ -387,7 +391,7 @@ __global__ __launch_bounds__(kLanes) void token_logprobs_kernel(const ScoreP a) 
     y.m = __shfl_xor(z.m, o);
     y.s = __shfl_xor(z.s, o);
     y.w = __shfl_xor(z.w, o);
-    z = join(z, y, a.scale2);
+    z = join(z, y, a.scale4);
   }
   if (threadIdx.x == 0) put_row(a, row, z, x_token, there);
   if constexpr (TOP) {
@@ -499,8 +503,8 @@ extern "C" int tsd_token_logprobs_static(const void* logits_dev, int32_t dtype, 
   a.V = V;
   a.top = top;
   a.wide = token_bytes == 8;
-  a.inv = (float)(1.0 / temperature);
-  a.scale2 = (float)(1.4426950408889634 / temperature);
+  a.inv4 = (float)(4.0 / temperature);
+  a.scale4 = (float)(4.0 * 1.4426950408889634 / temperature);
   a.logprobs = logprobs_dev;
   a.entropy = entropy_dev;
   a.top_ids = top_ids_dev;
