@@ -396,7 +396,8 @@ int tsd_verify_tree_static(const void* tokens_dev, const int32_t* parents_dev, i
 /* Rolls a cache back to a path through a tree: the keys and values in slot held_dev[b] + path_dev[b][i] go to slot held_dev[b] + i, for i = 0, 1, ..
  * as long as the path goes up (it ends at an entry that is not above the one before it, is negative, or not below N; tsd_verify_tree_static's ends
  * at -1).  n_layers caches that lie layer_stride elements apart in both pools (not 0 where there are several), as `cache` describes the first, share the page table.  A token whose
- * old or new slot is a hole stays where it is, the others move.  Pages that hold what is written must belong to one sequence.  N <= 256. */
+ * old or new slot is a hole stays where it is, the others move.  Pages that hold what is written must belong to one sequence.  N <= 256.
+ * k_dev may be v_dev (keys that are values: moved once); the pools' rows must not overlap otherwise. */
 int tsd_keep_path_static(const tsd_paged_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t B, int32_t N, const int32_t* held_dev,
                          const int32_t* path_dev, void* stream);
 

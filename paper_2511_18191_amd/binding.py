@@ -348,8 +348,8 @@ def verify_tree_static(tokens, parents, p=None, uniforms=None, choices=None, n_n
 def keep_path_static(k_pool, v_pool, page_table, held, path):
     """tsd_keep_path_static on torch's current stream of the tensors' device: in every sequence the keys and values of slots held + path[i] move to slots
     held + i.  Pools as for rope_append_static, or with the layers that share page_table as a first dimension, [layers, pages, page_tokens, kv_heads, head_dim];
-    held: int32 [B], the tokens held before the tree; path: int32 [B, N], as verify_tree_static gives it.  The pools are written in place.  No gradients, as for
-    rope_append_static."""
+    held: int32 [B], the tokens held before the tree; path: int32 [B, N], as verify_tree_static gives it.  The pools are written in place; k_pool may be
+    v_pool (keys that are values).  No gradients, as for rope_append_static."""
     if _tree_calls is None:
         _bind_tree_calls()
     rc = _tree_calls.keep_path_static(k_pool, v_pool, page_table, held, path)

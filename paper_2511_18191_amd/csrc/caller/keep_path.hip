@@ -2,7 +2,8 @@
 //
 // Slot held + path[i] goes to slot held + i.  A path goes up (parents come before their children), so that path[i] >= i: what is read for i lies at or
 // behind what is written for i, and only writes for later i reach it.  A lane takes one 16-byte column of the keys' or values' rows of a
-// (layer, sequence) for the whole path, reads before it writes, and nobody else touches its column: no order between lanes matters.
+// (layer, sequence) for the whole path, reads before it writes, and nobody else touches its column: no order between lanes matters.  (Where keys and values
+// are the same rows of one pool, they are moved once: two lanes would share a column.)
 //
 // Every byte is read and written once: memory bound, and for few tokens the trips to the path, the table and the rows.  Eight heads of 128, bf16: 4 rows of one
 // layer 3.0 us (a call 4.7), up to 8 rows of 64 sequences and 24 layers, 44 MB moved, 11.3 us (3.9 TB/s; a copy reaches 5.0 and would need 8.8).
@@ -17,11 +18,12 @@ struct KeepP {
   const int* held;
   const int* path;  // [B][N]
   int B, N, cols, per_head;  // 16-byte columns of a row of keys, and of one head
+  int all;                   // columns of keys and values
 };
 
 __global__ __launch_bounds__(256) void keep_path_kernel(const KeepP p) {
   typedef unsigned Words __attribute__((ext_vector_type(4)));
-  const int parts = (2 * p.cols + 255) / 256;
+  const int parts = (p.all + 255) / 256;
   unsigned i = blockIdx.x;
   const int part = i % parts;
   i /= parts;
@@ -33,7 +35,7 @@ __global__ __launch_bounds__(256) void keep_path_kernel(const KeepP p) {
   const bool values = col >= p.cols;
   const int c = values ? col - p.cols : col, head = c / p.per_head;
   char* pool = (values ? p.cache.v : p.cache.k) + layer * p.layer_stride + head * p.cache.head_stride + (c - head * p.per_head) * 16;
-  const bool live = col < 2 * p.cols;
+  const bool live = col < p.all;
   int before = -1;
   for (int base = 0; base < p.N; base += 64) {
     // 64 entries of the path at a time, as far as it goes up
@@ -96,7 +98,8 @@ extern "C" int tsd_keep_path_static(const tsd_paged_cache* cache, int32_t n_laye
   p.N = N;
   p.per_head = cache->head_dim * es / 16;
   p.cols = cache->n_kv_heads * p.per_head;
-  const int64_t parts = (2 * p.cols + 255) / 256;
+  p.all = cache->k_dev == cache->v_dev ? p.cols : 2 * p.cols;
+  const int64_t parts = (p.all + 255) / 256;
   if ((int64_t)B * n_layers > max_workgroups(256) / parts) return fail_no_handle(TSD_E_OUT_OF_RANGE, "more than 2^24 - 1 workgroups");
   keep_path_kernel<<<(unsigned)(parts * B * n_layers), 256, 0, (hipStream_t)stream>>>(p);
   const hipError_t e = hipGetLastError();
