@@ -7,6 +7,7 @@ paper_2511_18191_amd/libtsd.so and
 paper_2511_18191_amd/_torch_calls.so.
 """
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -26,7 +27,29 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", os.path.jo
          # no implicit FMA contraction: a*b + c is fused only where the source says fmaf(), so the
          # rounding of a row's arithmetic cannot depend on which unrolled copy of a loop body it met
          "-ffp-contract=off",
+         # what every kernel has of registers and memory, for _check_registers
+         "-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics",
          "-Wno-unused-command-line-argument"]
+REMARK = re.compile(r"remark: +(Function Name|AGPRs|VGPRs Spill): (\S+) \[-Rpass-analysis=kernel-resource-usage\]")
+
+
+def _check_registers(source, said):
+    """What the compiler said of a source, without its remarks on registers.  Raises where a kernel spills vector registers to memory while it has matrix
+    registers in use: a value of four registers that is kept half in the one and half in the other came back without a part (wrong scores of the fp32 attention
+    above 128 dims; ROCm 7.2), and nothing else shows it."""
+    kernels = []
+    for what, value in REMARK.findall(said):
+        if what == "Function Name":
+            kernels.append({"name": value})
+        else:
+            kernels[-1][what] = int(value)
+    with open(source) as f:
+        if "__global__" in f.read() and not kernels:
+            raise RuntimeError(f"{source}: the compiler said nothing of its kernels' registers")
+    bad = [k["name"] for k in kernels if k["AGPRs"] and k["VGPRs Spill"]]
+    if bad:
+        raise RuntimeError(f"{source}: spills vector registers to memory beside matrix registers in use, which has given wrong results: {', '.join(bad)}")
+    return "\n".join(l for l in said.splitlines() if "[-Rpass-analysis=kernel-resource-usage]" not in l)
 
 
 def _run(cmd):
@@ -57,7 +80,8 @@ def build_library(verbose=True):
 
     def one(pair):
         src, obj = pair
-        return _run([hipcc, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
+        at = os.path.join(CSRC, src)
+        return _check_registers(at, _run([hipcc, *FLAGS, "-c", at, "-o", obj]))
 
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
         for src, warn in zip(SOURCES, ex.map(one, zip(SOURCES, objs))):
