@@ -342,7 +342,8 @@ int tsd_verify_tokens_static(const void* draft_dev, const void* q_dev, const voi
 
 /* tsd_paged_attn_static for a model whose tokens see a window: token t of sequence b, at P = lens_dev[b] - n_new + t, sees the keys j <= P with
  * j > P - window or j < sinks (window >= 1, sinks >= 0).  Pages that no token sees any more may be holes.  What a call costs goes by the
- * keys that are seen, not by the cache's length.  Otherwise as tsd_paged_attn_static. */
+ * keys that are seen, not by the cache's length.  Otherwise as tsd_paged_attn_static.  (The parts of windows and trees take 256 MiB of workspace at most,
+ * and their slots 8 bytes a chunk and tile; what a call takes goes by max_len, B and T, and by what a window leaves: a max_len near the lengths keeps it small.) */
 int tsd_window_attn_workspace(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_len, int32_t window, int32_t sinks,
                               size_t* bytes_host);
 int tsd_window_attn_static(const tsd_paged_cache* cache, int32_t B, int32_t T, int32_t n_q_heads, const tsd_rows* q, const tsd_rows* out,

@@ -274,7 +274,8 @@ def paged_attn_static(q, k_pool, v_pool, page_table, lens, max_len=None, scale=N
 
 def window_attn_static(q, k_pool, v_pool, page_table, lens, window, sinks=0, max_len=None, scale=None, n_new=None, out=None, want_lse=False):
     """tsd_window_attn_static on torch's current stream of the tensors' device: as paged_attn_static, but a token at position P sees, of the keys up to its
-    own, the last `window` (its own among them) and the first `sinks`.  Pages of page_table that no token sees any more may hold -1."""
+    own, the last `window` (its own among them) and the first `sinks`.  Pages of page_table that no token sees any more may hold -1.  max_len (None: all that page_table
+    has room for) sizes the launch and its memory, which is 256 MiB at most where sequences are split: best a bound near the longest of lens."""
     if _tree_calls is None:
         _bind_tree_calls()
     if max_len is not None and max_len < 1:
@@ -292,7 +293,7 @@ def tree_attn_static(q, k_pool, v_pool, page_table, lens, parents, window=None, 
     """tsd_tree_attn_static on torch's current stream of the tensors' device: as paged_attn_static, but the last n_new (None: T each) tokens of every
     sequence are nodes of a tree, each of which sees the tokens before the tree, its ancestors and itself.  parents: int32 [B, T], or [T] for one tree
     in all sequences: the index of a node's parent, an earlier node; -1 for none.  window (None: all) and sinks as for window_attn_static, by positions: a
-    node's is lens - n_new + its depth.  T is at most 256."""
+    node's is lens - n_new + its depth.  T is at most 256.  max_len as for window_attn_static."""
     if _tree_calls is None:
         _bind_tree_calls()
     if max_len is not None and max_len < 1:

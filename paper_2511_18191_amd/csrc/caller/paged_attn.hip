@@ -368,6 +368,8 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // long as the tiles alone do not fill the card: 64 nodes over up to 16384 keys, 32 heads over 8 of 128, us with 512, 1024, 2048, 2752, 4096, 8192: 16 sequences 352, 307, 263,
 // 261, 297, 319; 4 sequences 109, 99, 92, 109, 135, 242; 2 sequences 62, 59, 75, 94, 132, 236; 1 sequence (256: 39) 41, 46, 72; 8 sequences of 16000 307, 258, 220,
 // 223, 210, 258; 32 sequences of up to 8000 410, 289, 275, 272, 299, 307; but 16 of up to 2000 79, 74, whole 68, 64 of up to 4096 444, 407, 386, whole 305.
+// Parts of windows and trees take 256 MiB at most: by keys alone, 16 trees of 64 nodes over up to 131072 had 806 MiB, 64 over up to 65536 838, and were no faster
+// (chunks of 2624 keys and of 8768: 2060 and 1995 us; of 5056 and 21888: 4016 and 3981; 4 of 256 nodes over up to 65536, of 2560 and 4416: 1071 and 1017).
 // In fp32, where products bound, and of lengths that windows make alike, tiles of 16 rows fill the card better up to 128 rows: 51 rows at a window of 500, 24
 // sequences, 4 heads of 80 34 us against 37, of 128 32 and 43, 200 sequences 118 and 168, but 256 rows, 16 sequences, 8 heads of 128, 307 and 247.
 struct AttnPlan {
@@ -384,6 +386,7 @@ struct AttnAsk {
   int parents_stride;
 };
 constexpr int kMostTokens = 1 << 30;
+constexpr int64_t kMostParts = 256 << 20;  // bytes of a call's parts, but for causal calls
 constexpr AttnAsk kAllKeys = {kCausal, kMostTokens, 0, nullptr, 0};
 
 AttnPlan attn_plan(const AttnAsk& ask, int dtype, int B, int T, int Hq, int Hkv, int D, int max_len) {
@@ -417,6 +420,10 @@ AttnPlan attn_plan(const AttnAsk& ask, int dtype, int B, int T, int Hq, int Hkv,
     chunk = (max_len + parts - 1) / parts;
   }
   chunk = std::max(chunk, least);
+  if (ask.mask != kCausal) {
+    const int64_t parts = std::max<int64_t>(1, kMostParts / ((int64_t)B * T * Hq * (D + 1) * 4));
+    chunk = std::max(chunk, (max_len + parts - 1) / parts);
+  }
   if (ask.mask != kCausal && max_len - chunk < chunk / 4) chunk = max_len;
   chunk = std::min<int64_t>(std::max(chunk, max_len * base / 16384), max_len);  // (a sequence that stays whole: no longer than it is)
   chunk = (chunk + step - 1) / step * step;
