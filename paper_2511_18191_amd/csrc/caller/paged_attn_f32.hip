@@ -171,15 +171,18 @@ __global__ __launch_bounds__(kAttnWaves * 64, DP <= 64 || (DP <= 96 && MT == 1) 
     for (int mt = 0; mt < MT; ++mt) {
       float s[8];
       unsigned live = valid;
-      if constexpr (M == kCausal)
-        live &= attn_bits(sees[mt].sees - sb);
-      else if (!whole)
-        live &= seen(sees[mt], sb);
+      if constexpr (M != kCausal)
+        if (!whole) live &= seen(sees[mt], sb);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s[j] = sc[mt][j >> 2][j & 3] * p.scale2;
         const int key = 16 * (j >> 2) + 4 * g + (j & 3);
-        if (!whole && !(live >> key & 1)) s[j] = -INFINITY;
+        // (a causal row's keys are compared: its bits, formed in every step, took one token of 64 sequences of up to 4000 keys, 12 heads over 4 of 64, from 59.7 us to 61.4)
+        if constexpr (M == kCausal) {
+          if (!whole && (!(live >> key & 1) || sb + key >= sees[mt].sees)) s[j] = -INFINITY;
+        } else {
+          if (!whole && !(live >> key & 1)) s[j] = -INFINITY;
+        }
       }
       const float alpha = attn_running_max(s, m_run[mt], e[mt]);
       float sum = 0.f;
