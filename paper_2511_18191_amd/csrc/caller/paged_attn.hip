@@ -361,17 +361,27 @@ hipError_t launch_dp(const PagedAttnP& p, int mt, int waves, hipStream_t st) {
 // 64 9.0 and 10.6; 32 of 20 rows of 128 47.5 and 39.3), and not for many rows (2 chunks of 128 rows of 64 24.5 and 15.4).
 // Wavefronts: four share a workgroup's keys, or, where there are workgroups enough and a few steps in all, one takes them (512 x 16 of 80 keys
 // 45.9 us, two 46.8, four 52.0).
+// The rules above were swept with causal calls, and windows and trees take them over; `least` holds a single sequence's tree at 256 keys a chunk, as it does
+// a causal call (26 nodes behind 1974 keys: 64 workgroups).
 // All of this goes by the places that a row tile may have, where windows leave fewer of them than max_len.  Windows make lengths alike, and a tree's rows are
 // many to join: their chunks are longer.  Few rows (us with 1024, some 3000 keys and whole): 64 tokens at a window of 4096, 32 heads over 8 of 128, 191, 190, 179,
 // 32 100, 96, 90, but 16 (2048) 53, 52, 66; trees of 8 nodes over up to 16384 keys, 16 sequences 154, 146 (2560: 140), 143 (8192), up to 3000 keys, 64 sequences 136, 121, 121; of
-// 64, 16 heads of 64, 296, 261, 246 (4096).  Trees of many rows: chunks for some 512 workgroups, of at most 2560 keys, as
+// 64, 16 heads of 64, 296, 261, 246 (4096).  Their border, 4608 places, lies between two sides that are close, but for few sequences: one token at a window, 32 heads
+// over 8 of 128, us in chunks of 1024, 2560, 4096 and whole, for 16, 32, 64 and 100 sequences: window 3000 40, 37, 37, 37; 87, 80, 80, 80; 154, 145, 146, 145; 243, 257,
+// 256, 256; 4096 50, 51, 54, 54; 116, 115, 108, 109; 207, 202, 197, 197; 326, 325, 346, 346; 5000 70, 64, 86, 87; 140, 137, 131, 131; 251, 246, 240, 240; 393, 400, 421,
+// 421; 8192 114, 122, 111, 144; 222, 219, 217, 211; 407, 398, 393, 387; 638, 623, 648, 686; 16384 221, 221, 213, 279; 440, 429, 426, 416; 799, 791, 779, 768; 1251,
+// 1230, 1238, 1367.  (Whole is best, by up to 7 %, where workgroups are a multiple of the compute units, at any window, and parts where they are not: the border
+// gives some of the one away above it, up to 5 %, and of the other below, up to 7 %.)  Trees of many rows: chunks for some 512 workgroups, of at most 2560 keys, as
 // long as the tiles alone do not fill the card: 64 nodes over up to 16384 keys, 32 heads over 8 of 128, us with 512, 1024, 2048, 2752, 4096, 8192: 16 sequences 352, 307, 263,
 // 261, 297, 319; 4 sequences 109, 99, 92, 109, 135, 242; 2 sequences 62, 59, 75, 94, 132, 236; 1 sequence (256: 39) 41, 46, 72; 8 sequences of 16000 307, 258, 220,
 // 223, 210, 258; 32 sequences of up to 8000 410, 289, 275, 272, 299, 307; but 16 of up to 2000 79, 74, whole 68, 64 of up to 4096 444, 407, 386, whole 305.
 // Parts of windows and trees take 256 MiB at most: by keys alone, 16 trees of 64 nodes over up to 131072 had 806 MiB, 64 over up to 65536 838, and were no faster
 // (chunks of 2624 keys and of 8768: 2060 and 1995 us; of 5056 and 21888: 4016 and 3981; 4 of 256 nodes over up to 65536, of 2560 and 4416: 1071 and 1017).
 // In fp32, where products bound, and of lengths that windows make alike, tiles of 16 rows fill the card better up to 128 rows: 51 rows at a window of 500, 24
-// sequences, 4 heads of 80 34 us against 37, of 128 32 and 43, 200 sequences 118 and 168, but 256 rows, 16 sequences, 8 heads of 128, 307 and 247.
+// sequences, 4 heads of 80 34 us against 37, of 128 32 and 43, 200 sequences 118 and 168, but 256 rows, 16 sequences, 8 heads of 128, 307 and 247.  Trees over whole
+// caches have the same rule, and it fits those of one sequence and short ones (us in tiles of 16 and 32 rows; 51 rows of 4 heads of 80: 1 sequence of 12000 keys 31, 34, 8
+// of up to 3000 46, 47, 24 of up to 500 30, 37), not many long ones, whose keys the tiles fetch anew (24 of up to 3000 132, 106; 27 rows of 4 heads of 128, 64 sequences, up
+// to 500 48, 38, 3000 237, 158, 12000 905, 583; of 64 96, 97 at 3000, 424, 314 at 12000; 128 rows of 8 of 128, 4 sequences, 12000 365, 345).
 struct AttnPlan {
   bool prompt;  // the kernel for many rows
   int mt, waves, row_tiles, splits, chunk, reach;

@@ -6,7 +6,8 @@
 // One token of 64 sequences of 2000 keys, 32 heads over 8 of 128: 185 us, 5.7 TB/s; 16 over 4 of 256: 182 us, 5.8.  2 x 1024 tokens behind 2048, 32 heads
 // over 8 of 128: 934 us, 92 of the 148 TFLOP/s that a large product reaches: keys and values are fetched for every 32 rows; 16 over 4 of 256: 1049 us, 82.
 // Short calls are bound by the matrix instructions of a step, 104 of 32 clocks for 80 dims, 128 for 128, and three trips to memory; heads of 80 and 96 dims have kernels of their own, two wavefronts of which share a SIMD
-// (3 tokens of 6 sequences of up to 1501 keys, 12 heads over 4 of 80: 17.2 us in the one for 128 dims, 15.6 so;
+// (12 heads over 4 of 80: 3 tokens of 6 sequences of up to 1501 keys, eight draws of lengths, 13.8 to 15.1 us in the one for 128 dims, 11.8 to 15.5 so, longer where one long sequence is
+// what a draw waits for; 5 tokens of 24 sequences 34.8 and 29.6, one of 64 of up to 4000 keys 167 and 105;
 // trees of up to 17 nodes of 24 such sequences at a window of 500 34).
 #include "paged_attn.h"
 

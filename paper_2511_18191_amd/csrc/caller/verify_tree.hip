@@ -5,8 +5,10 @@
 // the tree proposes, so that what is committed is distributed as the target's own.
 //
 // One row of p per step, each behind the one before it: a sequence's workgroup sums the row's segments (16 wavefronts), one of its wavefronts finds the
-// segment, the token and the child.  A step takes 2.2 us at 5000 fp32 probabilities, 3.2 at 32000, 4.3 at 50257 (and as much in bf16: conversions to 64 bits and
-// their sums, a quarter of a compute unit's rate each, are what grows); 26 nodes over 32000, walked 2 steps: 9.0 us, 64 trees of 32 over 50257, up to 5 steps: 24 us.
+// segment, the token and the child.  A step takes 2.2 us at 5000 fp32 probabilities, 3.2 at 32000, 4.3 at 50257: of its 9500 clocks there 5800 are the row, 201 KB
+// through one compute unit, 2900 the draw (the segment, its second read, two scans), 800 the child and barriers.  In bf16 the row, half the bytes, takes 5800 to 7800
+// clocks.  Sums in 32 bits would take 3 % off a call (4 % in bf16): conversions and additions in 64 bits are not what a step waits for.  26 nodes over 32000, walked
+// 2 steps: 8.9 us, 64 trees of 32 over 50257, up to 5 steps: 23 us, 16 of them 18, 256, one a compute unit and bound by memory too, 44.
 // (Elements looked at one by one 31 us; scans through LDS 30; all wavefronts finding the token for themselves 35.)  Where rows are few and long the
 // draws behind all nodes come first (draws_first).
 #include <algorithm>
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(WAVES * 64) void verify_tree_kernel(const TreeP a) 
   if (threadIdx.x == 0) a.n_acc[b] = n - 1;
 }
 
-constexpr int kMostWords = 1 << 21;  // of a vocabulary: the sums of a row's segments, twice, in LDS
+constexpr int kMostWords = 1 << 21;  // of a vocabulary: the sums of a row's segments, 16 KB, in LDS
 
 int check_tree(int dtype, int32_t B, int32_t N, int32_t V) {
   if (dtype != TSD_F32 && dtype != TSD_BF16) return fail_no_handle(TSD_E_INVALID_ARG, "dtype must be TSD_F32 or TSD_BF16");
